@@ -360,6 +360,61 @@ solar_status_t solar_lowrank_factor_static(int B, int M, int N, int d, int r, so
                                            const void* H, float* S, float* V, int* info,
                                            void* stream);
 
+/* ------------------------------------------------------------------------- *
+ * Linear attention with a decay per head: the history as a d x d state per head, the paper's
+ * Table 1 column beside SVD-attention (Eq. 8, MatMul(Query, MatMul(Key^T, Value))) with the weight on recent
+ * events that a state carried from event to event needs.
+ *
+ *   S_t = g S_{t-1} + k_t v_t^T    [d,d],      o_t = scale q_t S_t,      g = exp(log_decay[h])
+ *
+ * for t = 0 .. lengths[b] - 1, starting from state0 (S_{-1}).
+ *
+ *   Q, K, V    [B,T,H,d] dt (in)   *_strides: the strides of B, T and H in elements (three values on the HOST), or
+ *                                  NULL for a dense tensor; the last dimension is dense, and a stride is a
+ *                                  whole number of 16-byte pieces (0 repeats a row, inputs only)
+ *   log_decay  [H] f32      (in)   <= 0; 0 forgets nothing, -inf everything.  Not trained: no gradient.
+ *   scale                   (in)   multiplies the outputs
+ *   lengths    [B] int      (in)   events of each user, taken as 0 .. T; NULL: T.  Input rows behind a user's length
+ *                                  are not read, output rows behind it are zeros.
+ *   state0     [B,H,d,d] f32 (in)  S_{-1}, row i = component i of k; NULL: zeros
+ *   O          [B,T,H,d] dt (out)  rows may not lie over one another
+ *   state      [B,H,d,d] f32 (out) S_{lengths[b]-1}, or NULL.  May be state0 itself only in ..._step.
+ *
+ * One launch, no workspace; sums run in a fixed order, so results are reproducible bit for bit.  States and sums are
+ * fp32.  bf16 storage: the decayed scores and the state as an operand of q S are rounded to bf16 (the returned state is not).
+ * Inputs that are not finite make the outputs of their user and head NaN from there on.
+ * H <= 21845; T = 0 copies state0 to state.
+ * ------------------------------------------------------------------------- */
+solar_status_t solar_linear_attention_fwd(int B, int T, int H, int d, solar_dtype_t dt,
+                                          const void* Q, const long long* q_strides,
+                                          const void* K, const long long* k_strides,
+                                          const void* V, const long long* v_strides,
+                                          const float* log_decay, float scale, const int* lengths,
+                                          const float* state0, void* O, const long long* o_strides,
+                                          float* state, void* stream);
+
+/* Its backward pass: given dO = dL/dO and dstate = dL/dstate (NULL: zeros), the gradients of q, k, v and of
+ * state0 (dstate0, or NULL).  Everything else exactly as given to the forward call; the states are recomputed.
+ * Rows of dQ, dK and dV behind a user's length are zeros. */
+solar_status_t solar_linear_attention_bwd(int B, int T, int H, int d, solar_dtype_t dt,
+                                          const void* Q, const long long* q_strides,
+                                          const void* K, const long long* k_strides,
+                                          const void* V, const long long* v_strides,
+                                          const float* log_decay, float scale, const int* lengths,
+                                          const float* state0, const void* dO, const long long* do_strides,
+                                          const float* dstate, void* dQ, const long long* dq_strides,
+                                          void* dK, const long long* dk_strides, void* dV,
+                                          const long long* dv_strides, float* dstate0, void* stream);
+
+/* One event per user: `state` [B,H,d,d] f32 is updated in place and read.  Q, K, V, O [B,H,d] dt; *_strides: the
+ * strides of B and H in elements, or NULL for dense. */
+solar_status_t solar_linear_attention_step(int B, int H, int d, solar_dtype_t dt,
+                                           const void* Q, const long long* q_strides,
+                                           const void* K, const long long* k_strides,
+                                           const void* V, const long long* v_strides,
+                                           const float* log_decay, float scale, float* state,
+                                           void* O, const long long* o_strides, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,531 @@
+// Linear attention with a decay per head (the paper's Table 1 column beside SVD-attention, with the recency weight
+// that a state carried from event to event needs):
+//   S_t = g S_{t-1} + k_t v_t^T   [d,d],   o_t = scale q_t S_t,   g = exp(log_decay[h])
+// in chunks of C tokens, so that the products run on the tensor cores: with S the state before a chunk,
+//   o_t  = scale ( sum_{s <= t} g^(t-s) (q_t . k_s) v_s  +  g^(t+1) q_t S )        t, s within the chunk
+//   S   <- g^n S + sum_s g^(n-1-s) k_s v_s^T                                        n tokens in the chunk
+//
+// The backward pass is the same kernel in three roles.  With R_t = g R_{t+1} + scale q_t do_t^T (R_{T} from the
+// gradient of the last state),
+//   dq_t = scale S_t do_t              = forward(q := do, k := v, v := k), the state being S^T
+//   dk_t = R_t v_t                     = forward in reversed time (q := v, k := do, v := q), the state R^T
+//   dv_t = R_t^T k_t                   = forward in reversed time (q := k, k := q, v := do), the state R
+// and the gradient of the first state is g R_0.  In reversed time the state that comes in has no step of its own:
+// its weight is g^x, not g^(x+1) (`off`), and the same power goes into what a chunk adds.
+//
+// Long histories of few heads are cut into up to kMaxSegments segments whose CTAs form a cluster: each sums up its own
+// segment's state first (keys and values only), reads the others' through distributed shared memory, and then makes
+// its outputs.  So there is no workspace, no second launch and no order that changes between runs.
+//
+// Arithmetic: warp-level bf16 MMAs, fp32 accumulators; the state lives in fp32 accumulators over the whole segment.
+//   bf16 storage: q, k, v enter as they are; g^(n-1-s) k is split into a high and a low bf16 half (16 bits: the state is
+//   returned in fp32); the scores behind their decay and the state as an operand of q S are rounded to bf16, as the
+//   output will be.
+//   fp32 storage: every operand is split into three bf16 terms (24 bits), six products each: fp32's own rounding.
+#include <cuda_bf16.h>
+
+#include "sm100_ptx.cuh"
+#include "solar_internal.cuh"
+
+namespace solar {
+namespace {
+
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void ldsm(uint32_t (&x)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm_t(uint32_t (&x)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(addr) : "memory");
+}
+// 16 bytes to shared memory, zeros where `real` is false (the address is then not read)
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool real) {
+  const int n = real ? 16 : 0;
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+// (a, b) as NP pairs of bf16 whose sums are a and b, to 8 NP bits
+template <int NP> __device__ __forceinline__ void split(float a, float b, uint32_t (&w)[NP]) {
+#pragma unroll
+  for (int p = 0; p < NP; ++p) {
+    w[p] = ptx::pack_bf16(a, b);
+    a -= lo_f(w[p]);
+    b -= hi_f(w[p]);
+  }
+}
+
+template <typename T, int D> struct LaCfg {
+  static constexpr int NP = sizeof(T) == 2 ? 1 : 3;            // bf16 terms of an element
+  static constexpr int NA = sizeof(T) == 2 ? 2 : 3;            // of a decayed key
+  static constexpr int C = (NP == 3 && D == 128) ? 32 : 64;    // tokens of a chunk (fp32, d = 128: by shared memory)
+  static constexpr int NW = D == 128 ? 8 : 4, NT = NW * 32;
+  static constexpr int RW = C / 16, CW = NW / RW, OC = D / CW; // warps over rows and over columns of the output tile
+  static constexpr int MT = D / 16, NH = NW / MT, SC = D / NH; // warps over rows and over columns of the state
+  static constexpr int PITCH = 2 * D + 16;                     // bytes of a row: 16-byte pieces, no bank conflicts
+  static constexpr int TILE = C * PITCH, OPER = NP * TILE;     // one plane, one operand
+  static constexpr int STAGES = NP == 1 ? 2 : 1;
+  static constexpr int SBUF = NP == 1 ? 2 : 1;                 // copies of the state as an operand
+  static constexpr int STATE = NP * D * PITCH;
+  static constexpr int OFF_S = STAGES * 3 * OPER, OFF_W = OFF_S + SBUF * STATE;
+  static constexpr size_t SMEM = OFF_W + (C + 1) * sizeof(float);
+  static constexpr int PER_SM = SMEM <= 56 * 1024 ? 4 : SMEM <= 75 * 1024 ? 3 : SMEM <= 113 * 1024 ? 2 : 1;
+  static_assert(STAGES * 3 * OPER >= D * D * 4, "the segments' states lie over the tiles");
+};
+
+template <typename T, int D>
+__global__ void __launch_bounds__(LaCfg<T, D>::NT, LaCfg<T, D>::PER_SM > 3 ? 3 : LaCfg<T, D>::PER_SM)
+linear_attention_kernel(const __grid_constant__ LinearParams prm) {
+  using F = LaCfg<T, D>;
+  constexpr int C = F::C, NP = F::NP, NA = F::NA, NT = F::NT, PITCH = F::PITCH;
+  extern __shared__ __align__(16) uint8_t smem[];
+  const uint32_t sbase = ptx::smem_u32(smem);
+  float* sw = reinterpret_cast<float*>(smem + F::OFF_W);       // g^0 .. g^C
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, j = lane & 3;
+  const int seg = blockIdx.x, segs = gridDim.x;
+  const int h = blockIdx.y / prm.roles, b = blockIdx.z;
+  const LinearRole& R = prm.role[blockIdx.y % prm.roles];
+  const int rev = R.reverse;
+
+  pdl_wait();
+  const float l2 = ld_dep(prm.log_decay + h) * 1.4426950408889634f;
+  int len = prm.T;
+  if (prm.lengths != nullptr) len = min(max(ld_dep(prm.lengths + b), 0), prm.T);
+  auto power = [&](int n) { return n == 0 ? 1.f : exp2f((float)n * l2); };      // (0 * -inf: a head that forgets at once)
+  for (int i = tid; i <= C; i += NT) sw[i] = power(i);
+
+  const int chunks = (len + C - 1) / C, per = (chunks + segs - 1) / segs;
+  const int c0 = min(seg * per, chunks), c1 = min(c0 + per, chunks);
+  const T* qp = static_cast<const T*>(R.q.p) + (long long)b * R.q.sb + (long long)h * R.q.sh;
+  const T* kp = static_cast<const T*>(R.k.p) + (long long)b * R.k.sb + (long long)h * R.k.sh;
+  const T* vp = static_cast<const T*>(R.v.p) + (long long)b * R.v.sb + (long long)h * R.v.sh;
+  T* op = static_cast<T*>(R.o) + (long long)b * R.ob + (long long)h * R.oh;
+
+  // chunk c of an operand to shared memory: rows behind the sequence are zeros
+  auto load = [&](const T* p, long long st, int c, uint32_t dst) {
+    if constexpr (NP == 1) {
+      constexpr int PIECES = D / 8;
+#pragma unroll
+      for (int i = tid; i < C * PIECES; i += NT) {
+        const int x = i / PIECES, piece = i % PIECES, at = c * C + x;
+        const bool real = at < len;
+        const long long t = real ? (rev ? len - 1 - at : at) : 0;
+        cp_async16(dst + x * PITCH + piece * 16, p + t * st + piece * 8, real);
+      }
+    } else {
+      constexpr int PIECES = D / 4;
+#pragma unroll 4
+      for (int i = tid; i < C * PIECES; i += NT) {
+        const int x = i / PIECES, piece = i % PIECES, at = c * C + x;
+        float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (at < len) f = ld_dep(reinterpret_cast<const float4*>(p + (long long)(rev ? len - 1 - at : at) * st + piece * 4));
+        uint32_t w0[NP], w1[NP];
+        split<NP>(f.x, f.y, w0);
+        split<NP>(f.z, f.w, w1);
+#pragma unroll
+        for (int n = 0; n < NP; ++n)
+          *reinterpret_cast<uint2*>(smem + (dst - sbase) + n * F::TILE + x * PITCH + piece * 8) = make_uint2(w0[n], w1[n]);
+      }
+    }
+  };
+
+  // ---- the state: this warp's 16 rows x SC columns ---------------------------------------------------
+  const int mt = warp % F::MT, nh = warp / F::MT;
+  float st[F::SC / 8][4];
+#pragma unroll
+  for (int n = 0; n < F::SC / 8; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) st[n][i] = 0.f;
+  const int ldm_r = lane & 7, ldm_m = lane >> 3;
+  const uint32_t off_mn = (uint32_t)((((ldm_m >> 1) * 8 + ldm_r) * PITCH) + (ldm_m & 1) * 16);   // rows by bit 1, columns by bit 0
+  const uint32_t off_nm = (uint32_t)((((ldm_m & 1) * 8 + ldm_r) * PITCH) + (ldm_m >> 1) * 16);   // rows by bit 0, columns by bit 1
+
+  auto update = [&](uint32_t sk, uint32_t sv, int n_real) {
+    const float gn = sw[n_real];
+#pragma unroll
+    for (int n = 0; n < F::SC / 8; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) st[n][i] *= gn;
+#pragma unroll
+    for (int ks = 0; ks < C / 16; ++ks) {
+      float w[4];                                                  // of tokens 2j, 2j+1, 2j+8, 2j+9
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int s = ks * 16 + 2 * j + (i & 1) + (i >> 1) * 8;
+        w[i] = s < n_real ? R.ak * sw[n_real - 1 - s + rev] : 0.f;
+      }
+      uint32_t a[NA][4];
+      {
+        uint32_t x[NP][4];
+#pragma unroll
+        for (int p = 0; p < NP; ++p) ldsm_t(x[p], sk + p * F::TILE + ks * 16 * PITCH + mt * 32 + off_mn);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float u = lo_f(x[NP - 1][i]), v = hi_f(x[NP - 1][i]);
+#pragma unroll
+          for (int p = NP - 2; p >= 0; --p) { u += lo_f(x[p][i]); v += hi_f(x[p][i]); }
+          uint32_t y[NA];
+          split<NA>(u * w[(i >> 1) * 2], v * w[(i >> 1) * 2 + 1], y);
+#pragma unroll
+          for (int p = 0; p < NA; ++p) a[p][i] = y[p];
+        }
+      }
+#pragma unroll
+      for (int n2 = 0; n2 < F::SC / 16; ++n2)
+#pragma unroll
+        for (int pb = 0; pb < NP; ++pb) {
+          uint32_t y[4];
+          ldsm_t(y, sv + pb * F::TILE + ks * 16 * PITCH + (nh * F::SC + n2 * 16) * 2 + off_nm);
+#pragma unroll
+          for (int pa = 0; pa < NA; ++pa)
+            if (pa + pb < NA) {
+              mma(st[2 * n2], a[pa], y[0], y[1]);
+              mma(st[2 * n2 + 1], a[pa], y[2], y[3]);
+            }
+        }
+    }
+  };
+
+  const uint32_t tile0 = sbase;
+  auto oper = [&](int stage, int which) { return tile0 + (uint32_t)(stage * 3 + which) * F::OPER; };
+
+  // ---- the state before this segment ----------------------------------------------------------------
+  const size_t state_at = ((size_t)b * prm.H + h) * D * D;
+  auto state_row = [&](int i) { return mt * 16 + g + (i >> 1) * 8; };
+  auto state_col = [&](int n, int i) { return nh * F::SC + n * 8 + 2 * j + (i & 1); };
+  if (segs > 1) {
+    __syncthreads();
+    if (seg < segs - 1) {
+      if (NP == 1 && c0 < c1) { load(kp, R.k.st, c0, oper(0, 1)); load(vp, R.v.st, c0, oper(0, 2)); cp_async_commit(); }
+      for (int c = c0; c < c1; ++c) {
+        const int stage = NP == 1 ? (c - c0) & 1 : 0;
+        if constexpr (NP == 1) {
+          cp_async_wait<0>();
+          __syncthreads();
+          if (c + 1 < c1) { load(kp, R.k.st, c + 1, oper(stage ^ 1, 1)); load(vp, R.v.st, c + 1, oper(stage ^ 1, 2)); cp_async_commit(); }
+        } else {
+          __syncthreads();
+          load(kp, R.k.st, c, oper(0, 1)); load(vp, R.v.st, c, oper(0, 2));
+          __syncthreads();
+        }
+        update(oper(stage, 1), oper(stage, 2), min(C, len - c * C));
+      }
+      __syncthreads();
+      float4* mine = reinterpret_cast<float4*>(smem);
+#pragma unroll
+      for (int n = 0; n < F::SC / 8; ++n) mine[n * NT + tid] = make_float4(st[n][0], st[n][1], st[n][2], st[n][3]);
+    }
+    ptx::cluster_sync();
+#pragma unroll
+    for (int n = 0; n < F::SC / 8; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) st[n][i] = 0.f;
+    const int before = min(c0 * C, len);
+    for (int m = 0; m < seg; ++m) {                                // in the segments' order
+      const int end = min(min((m + 1) * per, chunks) * C, len);
+      const float f = power(before - end);
+      if (m * per >= chunks) break;
+#pragma unroll
+      for (int n = 0; n < F::SC / 8; ++n) {
+        const float4 e = ptx::ld_cluster_f4(reinterpret_cast<const float4*>(smem) + n * NT + tid, m);
+        st[n][0] = fmaf(f, e.x, st[n][0]); st[n][1] = fmaf(f, e.y, st[n][1]);
+        st[n][2] = fmaf(f, e.z, st[n][2]); st[n][3] = fmaf(f, e.w, st[n][3]);
+      }
+    }
+    ptx::cluster_sync();                                           // the tiles may be written again
+  }
+  if (R.s0 != nullptr) {
+    const float f = power(min(c0 * C, len));
+#pragma unroll
+    for (int n = 0; n < F::SC / 8; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        st[n][i] = fmaf(f, ld_dep(R.s0 + state_at + (size_t)state_row(i) * R.s0_r + (size_t)state_col(n, i) * R.s0_c), st[n][i]);
+  }
+
+  // The state as an operand: its accumulators rounded to NP bf16 terms
+  auto put_state = [&](int buf) {
+#pragma unroll
+    for (int n = 0; n < F::SC / 8; ++n)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        uint32_t y[NP];
+        split<NP>(st[n][2 * half], st[n][2 * half + 1], y);
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+          *reinterpret_cast<uint32_t*>(smem + F::OFF_S + buf * F::STATE + p * D * PITCH + state_row(2 * half) * PITCH + state_col(n, 0) * 2) = y[p];
+      }
+  };
+
+  // ---- outputs, chunk by chunk ------------------------------------------------------------------------
+  const int rw = warp % F::RW, cw = warp / F::RW;
+  if (c0 < c1) {
+    put_state(0);
+    if (NP == 1) {
+      load(qp, R.q.st, c0, oper(0, 0)); load(kp, R.k.st, c0, oper(0, 1)); load(vp, R.v.st, c0, oper(0, 2));
+      cp_async_commit();
+    }
+  }
+  for (int c = c0; c < c1; ++c) {
+    const int stage = NP == 1 ? (c - c0) & 1 : 0, buf = F::SBUF == 2 ? (c - c0) & 1 : 0;
+    if constexpr (NP == 1) {
+      cp_async_wait<0>();
+      __syncthreads();
+      if (c + 1 < c1) {
+        load(qp, R.q.st, c + 1, oper(stage ^ 1, 0)); load(kp, R.k.st, c + 1, oper(stage ^ 1, 1)); load(vp, R.v.st, c + 1, oper(stage ^ 1, 2));
+        cp_async_commit();
+      }
+    } else {
+      load(qp, R.q.st, c, oper(0, 0)); load(kp, R.k.st, c, oper(0, 1)); load(vp, R.v.st, c, oper(0, 2));
+      __syncthreads();
+    }
+    const uint32_t sq = oper(stage, 0), sk = oper(stage, 1), sv = oper(stage, 2), ss = sbase + F::OFF_S + buf * F::STATE;
+    const int n_real = min(C, len - c * C);
+
+    float o[F::OC / 8][4];
+#pragma unroll
+    for (int n = 0; n < F::OC / 8; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[n][i] = 0.f;
+    uint32_t q[NP][D / 16][4];
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) ldsm(q[p][ks], sq + p * F::TILE + rw * 16 * PITCH + ks * 32 + off_nm);
+    // q S, then its rows' powers
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+      for (int n2 = 0; n2 < F::OC / 16; ++n2)
+#pragma unroll
+        for (int pb = 0; pb < NP; ++pb) {
+          uint32_t y[4];
+          ldsm_t(y, ss + pb * D * PITCH + ks * 16 * PITCH + (cw * F::OC + n2 * 16) * 2 + off_nm);
+#pragma unroll
+          for (int pa = 0; pa < NP; ++pa)
+            if (pa + pb < NP) {
+              mma(o[2 * n2], q[pa][ks], y[0], y[1]);
+              mma(o[2 * n2 + 1], q[pa][ks], y[2], y[3]);
+            }
+        }
+    const int t0 = rw * 16 + g, t1 = t0 + 8;
+    {
+      const float f0 = R.aq * sw[t0 + 1 - rev], f1 = R.aq * sw[t1 + 1 - rev];
+#pragma unroll
+      for (int n = 0; n < F::OC / 8; ++n) { o[n][0] *= f0; o[n][1] *= f0; o[n][2] *= f1; o[n][3] *= f1; }
+    }
+    // scores of 16 keys at a time, decayed, times their values
+#pragma unroll
+    for (int kt = 0; kt < C / 16; ++kt) {
+      if (kt > rw) break;
+      float p0[4] = {0.f, 0.f, 0.f, 0.f}, p1[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+        for (int pb = 0; pb < NP; ++pb) {
+          uint32_t y[4];
+          ldsm(y, sk + pb * F::TILE + kt * 16 * PITCH + ks * 32 + off_mn);
+#pragma unroll
+          for (int pa = 0; pa < NP; ++pa)
+            if (pa + pb < NP) {
+              mma(p0, q[pa][ks], y[0], y[1]);
+              mma(p1, q[pa][ks], y[2], y[3]);
+            }
+        }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int t = (i >> 1) ? t1 : t0, s0 = kt * 16 + 2 * j + (i & 1), s1 = s0 + 8;
+        p0[i] = t >= s0 ? p0[i] * (R.ap * sw[t - s0]) : 0.f;
+        p1[i] = t >= s1 ? p1[i] * (R.ap * sw[t - s1]) : 0.f;
+      }
+      uint32_t a[NP][4];
+      {
+        uint32_t y[NP];
+        split<NP>(p0[0], p0[1], y);
+#pragma unroll
+        for (int p = 0; p < NP; ++p) a[p][0] = y[p];
+        split<NP>(p0[2], p0[3], y);
+#pragma unroll
+        for (int p = 0; p < NP; ++p) a[p][1] = y[p];
+        split<NP>(p1[0], p1[1], y);
+#pragma unroll
+        for (int p = 0; p < NP; ++p) a[p][2] = y[p];
+        split<NP>(p1[2], p1[3], y);
+#pragma unroll
+        for (int p = 0; p < NP; ++p) a[p][3] = y[p];
+      }
+#pragma unroll
+      for (int n2 = 0; n2 < F::OC / 16; ++n2)
+#pragma unroll
+        for (int pb = 0; pb < NP; ++pb) {
+          uint32_t y[4];
+          ldsm_t(y, sv + pb * F::TILE + kt * 16 * PITCH + (cw * F::OC + n2 * 16) * 2 + off_nm);
+#pragma unroll
+          for (int pa = 0; pa < NP; ++pa)
+            if (pa + pb < NP) {
+              mma(o[2 * n2], a[pa], y[0], y[1]);
+              mma(o[2 * n2 + 1], a[pa], y[2], y[3]);
+            }
+        }
+    }
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int at = c * C + (half ? t1 : t0);
+      if (at < len) {
+        T* row = op + (long long)(rev ? len - 1 - at : at) * R.ot + cw * F::OC + 2 * j;
+#pragma unroll
+        for (int n = 0; n < F::OC / 8; ++n) {
+          if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t*>(row + n * 8) = ptx::pack_bf16(o[n][2 * half], o[n][2 * half + 1]);
+          else *reinterpret_cast<float2*>(row + n * 8) = make_float2(o[n][2 * half], o[n][2 * half + 1]);
+        }
+      }
+    }
+    update(sk, sv, n_real);
+    if (c + 1 < c1) {
+      if constexpr (F::SBUF == 1) __syncthreads();                 // everybody has read the state before
+      put_state(F::SBUF == 2 ? buf ^ 1 : 0);
+    }
+    if constexpr (NP != 1) __syncthreads();                        // the tiles may be written again
+  }
+
+  // ---- the last state, and the rows behind the sequence -----------------------------------------------
+  if (R.s1 != nullptr && seg == segs - 1) {
+#pragma unroll
+    for (int n = 0; n < F::SC / 8; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) R.s1[state_at + (size_t)state_row(i) * D + state_col(n, i)] = st[n][i];
+  }
+  constexpr int PIECES = D * (int)sizeof(T) / 16;
+  for (long long i = (long long)seg * NT + tid; i < (long long)(prm.T - len) * PIECES; i += (long long)segs * NT)
+    *reinterpret_cast<uint4*>(op + (len + i / PIECES) * R.ot + (i % PIECES) * (16 / sizeof(T))) = make_uint4(0, 0, 0, 0);
+}
+
+constexpr int kMaxSegments = 8;      // CTAs of a cluster
+
+// Segments per (user, head): the fewest waves x chunks of a CTA, where the pass over the keys and values that a
+// segmented history needs first costs about half of the pass that makes the outputs.
+template <typename F> int linear_segments(long long ctas, int T) {
+  const int chunks = (T + F::C - 1) / F::C;
+  const long long slots = (long long)kNumSMs * F::PER_SM;
+  long long best = -1;
+  int segs = 1;
+  for (int s = 1; s <= kMaxSegments && s <= chunks; s *= 2) {
+    const long long waves = (ctas * s + slots - 1) / slots;
+    const long long per = (chunks + s - 1) / s, cost = waves * (s > 1 ? 3 * per + 4 : 2 * per);
+    if (best < 0 || cost < best) { best = cost; segs = s; }
+  }
+  return segs;
+}
+
+template <typename T, int D> cudaError_t launch_td(const LinearParams& prm, int B, cudaStream_t st) {
+  using F = LaCfg<T, D>;
+  static bool limits_set[kMaxDevicesCached] = {};
+  const cudaError_t e = set_kernel_limits(reinterpret_cast<const void*>(&linear_attention_kernel<T, D>), F::SMEM, limits_set);
+  if (e != cudaSuccess) return e;
+  const int segs = linear_segments<F>((long long)B * prm.H * prm.roles, prm.T);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(segs, prm.H * prm.roles, B);
+  cfg.blockDim = dim3(F::NT);
+  cfg.dynamicSmemBytes = F::SMEM;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = segs; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = segs > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, linear_attention_kernel<T, D>, prm);
+}
+
+// ---- one event ------------------------------------------------------------------------------------------
+// S <- g S + k v^T, o = scale q S: 32 columns of one state per CTA, 256 threads as 32 row threads x 8 pieces of four
+// columns.  Bound by the state's bytes, once in and once out; every thread's rows are loaded before the first is used.
+template <typename T, int D>
+__global__ void __launch_bounds__(256)
+linear_step_kernel(LinearOperand q, LinearOperand k, LinearOperand v, const float* __restrict__ log_decay, float scale,
+                   float* state, T* o, long long ob, long long oh, int H) {
+  constexpr int ROWS = D / 32;
+  __shared__ float4 part[8][8];
+  const int tid = threadIdx.x, col = tid & 7, row = tid >> 3, warp = tid >> 5, lane = tid & 31;
+  const int h = blockIdx.y, b = blockIdx.z, c0 = blockIdx.x * 32 + col * 4;
+  pdl_wait();
+  float4* S = reinterpret_cast<float4*>(state + ((size_t)b * H + h) * D * D + c0) ;
+  float4 s[ROWS];
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) s[i] = ld_dep(S + (size_t)(row + 32 * i) * (D / 4));
+  const T* qp = static_cast<const T*>(q.p) + (long long)b * q.sb + (long long)h * q.sh;
+  const T* kp = static_cast<const T*>(k.p) + (long long)b * k.sb + (long long)h * k.sh;
+  const T* vp = static_cast<const T*>(v.p) + (long long)b * v.sb + (long long)h * v.sh;
+  const float gm = expf(ld_dep(log_decay + h));
+  const float v0 = to_f32(vp[c0]), v1 = to_f32(vp[c0 + 1]), v2 = to_f32(vp[c0 + 2]), v3 = to_f32(vp[c0 + 3]);
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    const float kk = to_f32(kp[row + 32 * i]), qq = to_f32(qp[row + 32 * i]);
+    s[i].x = fmaf(kk, v0, gm * s[i].x); s[i].y = fmaf(kk, v1, gm * s[i].y);
+    s[i].z = fmaf(kk, v2, gm * s[i].z); s[i].w = fmaf(kk, v3, gm * s[i].w);
+    acc.x = fmaf(qq, s[i].x, acc.x); acc.y = fmaf(qq, s[i].y, acc.y);
+    acc.z = fmaf(qq, s[i].z, acc.z); acc.w = fmaf(qq, s[i].w, acc.w);
+    S[(size_t)(row + 32 * i) * (D / 4)] = s[i];
+  }
+#pragma unroll
+  for (int m = 8; m < 32; m <<= 1) {
+    acc.x += __shfl_xor_sync(~0u, acc.x, m); acc.y += __shfl_xor_sync(~0u, acc.y, m);
+    acc.z += __shfl_xor_sync(~0u, acc.z, m); acc.w += __shfl_xor_sync(~0u, acc.w, m);
+  }
+  if (lane < 8) part[warp][lane] = acc;
+  __syncthreads();
+  if (tid < 32) {
+    const float* p = reinterpret_cast<const float*>(part) + tid;
+    float x = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) x += p[w * 32];
+    o[(long long)b * ob + (long long)h * oh + blockIdx.x * 32 + tid] = from_f32<T>(scale * x);
+  }
+}
+
+template <typename T, int D>
+cudaError_t launch_step_td(int B, int H, const LinearOperand& q, const LinearOperand& k, const LinearOperand& v,
+                           const float* log_decay, float scale, float* state, void* o, long long ob, long long oh, cudaStream_t st) {
+  return launch_pdl(linear_step_kernel<T, D>, dim3(D / 32, H, B), dim3(256), 0, st, q, k, v, log_decay, scale, state,
+                    static_cast<T*>(o), ob, oh, H);
+}
+
+}  // namespace
+
+cudaError_t launch_linear_attention(int B, int d, solar_dtype_t dt, const LinearParams& prm, cudaStream_t st) {
+  if (dt == SOLAR_BF16) {
+    if (d == 32) return launch_td<__nv_bfloat16, 32>(prm, B, st);
+    if (d == 64) return launch_td<__nv_bfloat16, 64>(prm, B, st);
+    return launch_td<__nv_bfloat16, 128>(prm, B, st);
+  }
+  if (d == 32) return launch_td<float, 32>(prm, B, st);
+  if (d == 64) return launch_td<float, 64>(prm, B, st);
+  return launch_td<float, 128>(prm, B, st);
+}
+
+cudaError_t launch_linear_step(int B, int H, int d, solar_dtype_t dt, const LinearOperand& q, const LinearOperand& k,
+                               const LinearOperand& v, const float* log_decay, float scale, float* state, void* o,
+                               long long ob, long long oh, cudaStream_t st) {
+#define SOLAR_STEP(TT, DD) return launch_step_td<TT, DD>(B, H, q, k, v, log_decay, scale, state, o, ob, oh, st)
+  if (dt == SOLAR_BF16) {
+    if (d == 32) SOLAR_STEP(__nv_bfloat16, 32);
+    if (d == 64) SOLAR_STEP(__nv_bfloat16, 64);
+    SOLAR_STEP(__nv_bfloat16, 128);
+  }
+  if (d == 32) SOLAR_STEP(float, 32);
+  if (d == 64) SOLAR_STEP(float, 64);
+  SOLAR_STEP(float, 128);
+#undef SOLAR_STEP
+}
+
+}  // namespace solar

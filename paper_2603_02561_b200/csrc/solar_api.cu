@@ -71,6 +71,56 @@ solar_status_t eig_impl(int B, int d, int r, solar_dtype_t dt, int route, int sw
                               plan.parts, plan.splits, gsum, S, V, info, route_taken, st));
 }
 
+// A token tensor [B,T,H,d]: strides of the first three dimensions in elements (NULL: dense), whole 16-byte pieces.
+struct Tokens {
+  long long sb, st, sh;
+};
+solar_status_t token_strides(int B, int T, int H, int d, solar_dtype_t dt, const void* p, const long long* strides, Tokens* out) {
+  SOLAR_TRY(check_ptr(p));
+  if (strides == nullptr) {
+    *out = {(long long)T * H * d, (long long)H * d, d};
+    return SOLAR_OK;
+  }
+  *out = {strides[0], strides[1], strides[2]};
+  const long long piece = 16 / (long long)elem_size(dt);
+  const long long n[3] = {B, T, H};
+  for (int i = 0; i < 3; ++i)
+    if (strides[i] < 0 || (n[i] > 1 && strides[i] % piece != 0)) return SOLAR_ERR_INVALID_ARG;
+  return SOLAR_OK;
+}
+solar_status_t token_input(int B, int T, int H, int d, solar_dtype_t dt, const void* p, const long long* strides, LinearOperand* out) {
+  Tokens t;
+  SOLAR_TRY(token_strides(B, T, H, d, dt, p, strides, &t));
+  *out = {p, t.sb, t.st, t.sh};
+  return SOLAR_OK;
+}
+// An output's rows may not lie over one another: each dimension steps over all of the smaller ones.
+solar_status_t token_output(int B, int T, int H, int d, solar_dtype_t dt, const void* p, const long long* strides, Tokens* out) {
+  SOLAR_TRY(token_strides(B, T, H, d, dt, p, strides, out));
+  long long n[3] = {B, T, H}, s[3] = {out->sb, out->st, out->sh};
+  for (int i = 0; i < 3; ++i)
+    for (int k = i + 1; k < 3; ++k)
+      if (s[k] < s[i]) { const long long a = s[i], c = n[i]; s[i] = s[k]; n[i] = n[k]; s[k] = a; n[k] = c; }
+  long long extent = d;
+  for (int i = 0; i < 3; ++i) {
+    if (n[i] <= 1) continue;
+    if (s[i] < extent) return SOLAR_ERR_INVALID_ARG;
+    extent += (n[i] - 1) * s[i];
+  }
+  return SOLAR_OK;
+}
+solar_status_t check_linear(int B, int T, int H, int d, solar_dtype_t dt) {
+  if (dt != SOLAR_F32 && dt != SOLAR_BF16) return SOLAR_ERR_UNSUPPORTED;
+  if (B < 0 || T < 0 || H < 1) return SOLAR_ERR_INVALID_ARG;
+  if (d != 32 && d != 64 && d != 128) return SOLAR_ERR_UNSUPPORTED;
+  if (B > 65535 || H > 65535 / 3) return SOLAR_ERR_UNSUPPORTED;
+  return SOLAR_OK;
+}
+solar_status_t check_optional(const void* p, unsigned align) {
+  return (reinterpret_cast<uintptr_t>(p) & (align - 1)) == 0 ? SOLAR_OK : SOLAR_ERR_INVALID_ARG;
+}
+solar_status_t check_word_ptr(const void* p) { return p == nullptr ? SOLAR_ERR_INVALID_ARG : check_optional(p, 4); }
+
 }  // namespace
 
 extern "C" {
@@ -355,6 +405,98 @@ solar_status_t solar_factored_softmax_attention_fwd(int B, int M, int N, int d, 
   SOLAR_TRY(from_cuda(launch_attn_prepare(B, d, r, dt, nullptr, V, Wq, Wk, Wv, scale * 1.4426950408889634f, ws, lay, false,
                                           nullptr, st, counters, split.items_per_user)));
   return from_cuda(launch_flash_factored(B, M, N, d, r, C, US, O, ws, lay, split, st));
+}
+
+solar_status_t solar_linear_attention_fwd(int B, int T, int H, int d, solar_dtype_t dt, const void* Q, const long long* q_strides,
+                                          const void* K, const long long* k_strides, const void* V, const long long* v_strides,
+                                          const float* log_decay, float scale, const int* lengths, const float* state0,
+                                          void* O, const long long* o_strides, float* state, void* stream) {
+  SOLAR_TRY(check_linear(B, T, H, d, dt));
+  if (B == 0) return SOLAR_OK;
+  LinearParams prm = {};
+  prm.roles = 1; prm.T = T; prm.H = H; prm.lengths = lengths; prm.log_decay = log_decay;
+  LinearRole& r = prm.role[0];
+  if (T > 0) {
+    SOLAR_TRY(token_input(B, T, H, d, dt, Q, q_strides, &r.q));
+    SOLAR_TRY(token_input(B, T, H, d, dt, K, k_strides, &r.k));
+    SOLAR_TRY(token_input(B, T, H, d, dt, V, v_strides, &r.v));
+    Tokens o;
+    SOLAR_TRY(token_output(B, T, H, d, dt, O, o_strides, &o));
+    r.o = O; r.ob = o.sb; r.ot = o.st; r.oh = o.sh;
+  }
+  SOLAR_TRY(check_word_ptr(log_decay));
+  SOLAR_TRY(check_optional(lengths, 4));
+  SOLAR_TRY(check_optional(state0, 16));
+  SOLAR_TRY(check_optional(state, 16));
+  if (state != nullptr && state == state0) return SOLAR_ERR_INVALID_ARG;       // other segments still read it
+  if (T == 0 && state == nullptr) return SOLAR_OK;
+  r.s0 = state0; r.s0_r = d; r.s0_c = 1; r.s1 = state;
+  r.ap = scale; r.aq = scale; r.ak = 1.f;
+  return from_cuda(launch_linear_attention(B, d, dt, prm, static_cast<cudaStream_t>(stream)));
+}
+
+solar_status_t solar_linear_attention_bwd(int B, int T, int H, int d, solar_dtype_t dt, const void* Q, const long long* q_strides,
+                                          const void* K, const long long* k_strides, const void* V, const long long* v_strides,
+                                          const float* log_decay, float scale, const int* lengths, const float* state0,
+                                          const void* dO, const long long* do_strides, const float* dstate,
+                                          void* dQ, const long long* dq_strides, void* dK, const long long* dk_strides,
+                                          void* dV, const long long* dv_strides, float* dstate0, void* stream) {
+  SOLAR_TRY(check_linear(B, T, H, d, dt));
+  if (B == 0) return SOLAR_OK;
+  LinearOperand q = {}, k = {}, v = {}, g = {};
+  Tokens out[3] = {};
+  if (T > 0) {
+    SOLAR_TRY(token_input(B, T, H, d, dt, Q, q_strides, &q));
+    SOLAR_TRY(token_input(B, T, H, d, dt, K, k_strides, &k));
+    SOLAR_TRY(token_input(B, T, H, d, dt, V, v_strides, &v));
+    SOLAR_TRY(token_input(B, T, H, d, dt, dO, do_strides, &g));
+    SOLAR_TRY(token_output(B, T, H, d, dt, dQ, dq_strides, &out[0]));
+    SOLAR_TRY(token_output(B, T, H, d, dt, dK, dk_strides, &out[1]));
+    SOLAR_TRY(token_output(B, T, H, d, dt, dV, dv_strides, &out[2]));
+  }
+  SOLAR_TRY(check_word_ptr(log_decay));
+  SOLAR_TRY(check_optional(lengths, 4));
+  SOLAR_TRY(check_optional(state0, 16));
+  SOLAR_TRY(check_optional(dstate, 16));
+  SOLAR_TRY(check_optional(dstate0, 16));
+  if (dstate0 != nullptr && (dstate0 == dstate || dstate0 == state0)) return SOLAR_ERR_INVALID_ARG;
+  if (T == 0 && dstate0 == nullptr) return SOLAR_OK;
+  LinearParams prm = {};
+  prm.roles = 3; prm.T = T; prm.H = H; prm.lengths = lengths; prm.log_decay = log_decay;
+  auto role = [&](int i, const LinearOperand& a, const LinearOperand& b, const LinearOperand& c, void* o, const float* s0, bool transposed) {
+    LinearRole& r = prm.role[i];
+    r.q = a; r.k = b; r.v = c;
+    r.o = o; r.ob = out[i].sb; r.ot = out[i].st; r.oh = out[i].sh;
+    r.s0 = s0; r.s0_r = transposed ? 1 : d; r.s0_c = transposed ? d : 1;
+    r.reverse = i > 0; r.ap = scale; r.aq = i > 0 ? 1.f : scale; r.ak = i > 0 ? scale : 1.f;
+  };
+  role(0, g, v, k, dQ, state0, true);
+  role(1, v, g, q, dK, dstate, true);
+  role(2, k, q, g, dV, dstate, false);
+  prm.role[2].s1 = dstate0;
+  return from_cuda(launch_linear_attention(B, d, dt, prm, static_cast<cudaStream_t>(stream)));
+}
+
+solar_status_t solar_linear_attention_step(int B, int H, int d, solar_dtype_t dt, const void* Q, const long long* q_strides,
+                                           const void* K, const long long* k_strides, const void* V, const long long* v_strides,
+                                           const float* log_decay, float scale, float* state, void* O, const long long* o_strides,
+                                           void* stream) {
+  SOLAR_TRY(check_linear(B, 1, H, d, dt));
+  if (B == 0) return SOLAR_OK;
+  LinearOperand op[3];
+  const void* in[3] = {Q, K, V};
+  const long long* strides[3] = {q_strides, k_strides, v_strides};
+  for (int i = 0; i < 3; ++i) {
+    const long long s[3] = {strides[i] ? strides[i][0] : 0, 0, strides[i] ? strides[i][1] : 0};
+    SOLAR_TRY(token_input(B, 1, H, d, dt, in[i], strides[i] ? s : nullptr, &op[i]));
+  }
+  Tokens o;
+  const long long s[3] = {o_strides ? o_strides[0] : 0, 0, o_strides ? o_strides[1] : 0};
+  SOLAR_TRY(token_output(B, 1, H, d, dt, O, o_strides ? s : nullptr, &o));
+  SOLAR_TRY(check_word_ptr(log_decay));
+  SOLAR_TRY(check_ptr(state));
+  return from_cuda(launch_linear_step(B, H, d, dt, op[0], op[1], op[2], log_decay, scale, state, O, o.sb, o.sh,
+                                      static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -252,6 +252,35 @@ cudaError_t launch_attn_pipe(int B, int M, int r, const void* C, unsigned flags,
 cudaError_t launch_attn_umma(int B, int M, int d, int r, const void* C, unsigned flags, void* O,
                              const char* ws, const AttnWs& lay, bool early_c, cudaStream_t st);
 
+// Linear attention (csrc/linear_attention.cu).  Token tensors [B,T,H,d] with strides in elements, innermost dense.
+struct LinearOperand {
+  const void* p;
+  long long sb, st, sh;
+};
+// One pass o = scores(q, k) v over a history, forward or in reversed time.  The state that comes in is element
+// (i, j) at s0[i * s0_r + j * s0_c] of a user's head (nullptr: zero), the last state goes to s1 (nullptr: nowhere).
+// ap, aq, ak: factors of the scores, of q S, and of what is added to the state.
+struct LinearRole {
+  LinearOperand q, k, v;
+  void* o;
+  long long ob, ot, oh;
+  const float* s0;
+  int s0_r, s0_c;
+  float* s1;
+  int reverse;
+  float ap, aq, ak;
+};
+struct LinearParams {
+  LinearRole role[3];
+  int roles, T, H;
+  const int* lengths;
+  const float* log_decay;
+};
+cudaError_t launch_linear_attention(int B, int d, solar_dtype_t dt, const LinearParams& prm, cudaStream_t st);
+cudaError_t launch_linear_step(int B, int H, int d, solar_dtype_t dt, const LinearOperand& q, const LinearOperand& k,
+                               const LinearOperand& v, const float* log_decay, float scale, float* state, void* o,
+                               long long ob, long long oh, cudaStream_t st);
+
 // ---- per-kernel launch limits -----------------------------------------------------------------
 // Raises a kernel's dynamic shared-memory limit and asks for the largest shared-memory carve-out
 // (an SM keeps ONE carve-out at a time: kernels of several requests share an SM only if they

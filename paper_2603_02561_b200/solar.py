@@ -57,6 +57,9 @@ SIGNATURES = {
     "solar_static_scratch_bytes": (_c_size, []),
     "solar_lowrank_factor_static": (_c_int, [_c_int] * 5 + [_c_int] + [_c_vp] * 4 + [_c_vp]),
     "solar_attn_apply": (_c_int, [_c_int] * 4 + [_c_int, _c_vp, _c_uint, _c_vp, _c_vp, _c_size, _c_vp]),
+    "solar_linear_attention_fwd": (_c_int, [_c_int] * 4 + [_c_int] + [_c_vp] * 6 + [_c_vp, _c_float] + [_c_vp] * 6),
+    "solar_linear_attention_bwd": (_c_int, [_c_int] * 4 + [_c_int] + [_c_vp] * 6 + [_c_vp, _c_float] + [_c_vp] * 13),
+    "solar_linear_attention_step": (_c_int, [_c_int] * 3 + [_c_int] + [_c_vp] * 6 + [_c_vp, _c_float] + [_c_vp] * 4),
 }
 
 _lib = None
@@ -112,6 +115,13 @@ def _stream(stream=None):
     if _raw_stream is not None:
         return _raw_stream(_current_device())
     return torch.cuda.current_stream().cuda_stream
+
+
+def _stream_on(device, stream=None):
+    """The stream of a call whose tensors are on `device`, which has to be the current one: a launch goes there."""
+    if device.index is not None and _current_device is not None and device.index != _current_device():
+        raise ValueError(f"tensors on {device}, but the current device is cuda:{_current_device()}")
+    return _stream(stream)
 
 
 def _check(status: int, where: str):
@@ -419,3 +429,94 @@ def forward(H, C, Wq, Wk, Wv, r, scale, flags=0, workspace=None, stream=None):
     S, V = lowrank_factor(H, r, workspace=workspace, M=M, stream=stream)
     O = svd_attention_fwd(C, S, V, Wq, Wk, Wv, scale, flags, workspace=workspace, N=N, stream=stream)
     return O, S, V
+
+
+# ---- linear attention with a decay per head ------------------------------------------------------
+def _strides(t, name, shape, dtype, device):
+    """A token tensor's strides for the library: None where it is dense."""
+    if t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_cuda:
+        raise ValueError(f"{name}: want {dtype} {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if t.is_contiguous():
+        return None
+    if t.stride(-1) != 1:
+        raise ValueError(f"{name}: the last dimension has to be dense, got strides {t.stride()}")
+    return (ctypes.c_longlong * 3)(*t.stride()[:-1])
+
+
+def _need_on(t, shape, dtype, name, device):
+    _need(t, shape, dtype, name)
+    if t.device != device:
+        raise ValueError(f"{name}: want it on {device}, got {t.device}")
+
+
+def _tokens_like(t):
+    return _empty(t.shape, dtype=t.dtype, device=t.device)
+
+
+def linear_attention_fwd(q, k, v, log_decay, scale, state0=None, lengths=None, O=None, state=None, stream=None):
+    """solar_linear_attention_fwd: q, k, v [B,T,H,d] (any strides with a dense last dimension) -> O [B,T,H,d] and the
+    last state [B,H,d,d] fp32."""
+    B, T, H, d = q.shape
+    dt, dev, shape = q.dtype, q.device, q.shape
+    ss = [_strides(t, n, shape, dt, dev) for t, n in ((q, "q"), (k, "k"), (v, "v"))]
+    _need_on(log_decay, (H,), _F32, "log_decay", dev)
+    if lengths is not None:
+        _need_on(lengths, (B,), _I32, "lengths", dev)
+    if state0 is not None:
+        _need_on(state0, (B, H, d, d), _F32, "state0", dev)
+    if O is None:
+        O = _tokens_like(q)
+    so = _strides(O, "O", shape, dt, dev)
+    if state is None:
+        state = _empty((B, H, d, d), dtype=_F32, device=dev)
+    else:
+        _need_on(state, (B, H, d, d), _F32, "state", dev)
+    st = (_lib or lib()).solar_linear_attention_fwd(
+        B, T, H, d, dtype_code(dt), q.data_ptr(), ss[0], k.data_ptr(), ss[1], v.data_ptr(), ss[2], log_decay.data_ptr(), float(scale),
+        _ptr(lengths), _ptr(state0), O.data_ptr(), so, state.data_ptr(), _stream_on(dev, stream))
+    if st:
+        _check(st, "solar_linear_attention_fwd")
+    return O, state
+
+
+def linear_attention_bwd(q, k, v, log_decay, scale, dO, state0=None, dstate=None, lengths=None, dq=None, dk=None, dv=None,
+                         dstate0=None, stream=None):
+    """solar_linear_attention_bwd -> dq, dk, dv [B,T,H,d] and dstate0 [B,H,d,d] fp32."""
+    B, T, H, d = q.shape
+    dt, dev, shape = q.dtype, q.device, q.shape
+    si = [_strides(t, n, shape, dt, dev) for t, n in ((q, "q"), (k, "k"), (v, "v"), (dO, "dO"))]
+    _need_on(log_decay, (H,), _F32, "log_decay", dev)
+    if lengths is not None:
+        _need_on(lengths, (B,), _I32, "lengths", dev)
+    for t, n in ((state0, "state0"), (dstate, "dstate"), (dstate0, "dstate0")):
+        if t is not None:
+            _need_on(t, (B, H, d, d), _F32, n, dev)
+    dq, dk, dv = (_tokens_like(q) if t is None else t for t in (dq, dk, dv))
+    so = [_strides(t, n, shape, dt, dev) for t, n in ((dq, "dq"), (dk, "dk"), (dv, "dv"))]
+    if dstate0 is None:
+        dstate0 = _empty((B, H, d, d), dtype=_F32, device=dev)
+    st = (_lib or lib()).solar_linear_attention_bwd(
+        B, T, H, d, dtype_code(dt), q.data_ptr(), si[0], k.data_ptr(), si[1], v.data_ptr(), si[2], log_decay.data_ptr(), float(scale),
+        _ptr(lengths), _ptr(state0), dO.data_ptr(), si[3], _ptr(dstate), dq.data_ptr(), so[0], dk.data_ptr(), so[1],
+        dv.data_ptr(), so[2], dstate0.data_ptr(), _stream_on(dev, stream))
+    if st:
+        _check(st, "solar_linear_attention_bwd")
+    return dq, dk, dv, dstate0
+
+
+def linear_attention_step(q, k, v, log_decay, scale, state, O=None, stream=None):
+    """solar_linear_attention_step: one event per user, q, k, v [B,H,d]; `state` [B,H,d,d] fp32 is updated in place."""
+    B, H, d = q.shape
+    dt, dev, shape = q.dtype, q.device, q.shape
+    ss = [_strides(t, n, shape, dt, dev) for t, n in ((q, "q"), (k, "k"), (v, "v"))]
+    _need_on(log_decay, (H,), _F32, "log_decay", dev)
+    _need_on(state, (B, H, d, d), _F32, "state", dev)
+    if O is None:
+        O = _tokens_like(q)
+    so = _strides(O, "O", shape, dt, dev)
+    st = (_lib or lib()).solar_linear_attention_step(
+        B, H, d, dtype_code(dt), q.data_ptr(), ss[0], k.data_ptr(), ss[1], v.data_ptr(), ss[2], log_decay.data_ptr(), float(scale),
+        state.data_ptr(), O.data_ptr(), so, _stream_on(dev, stream))
+    if st:
+        _check(st, "solar_linear_attention_step")
+    return O
