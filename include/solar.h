@@ -415,6 +415,52 @@ solar_status_t solar_linear_attention_step(int B, int H, int d, solar_dtype_t dt
                                            const float* log_decay, float scale, float* state,
                                            void* O, const long long* o_strides, void* stream);
 
+/* ------------------------------------------------------------------------- *
+ * A user's history kept in 8 bits between requests, and softmax attention over it (Eq. 6-7; Table 1's first column):
+ * what a serving process keeps where the history itself, not its rank-r factors, has to be attended over.
+ *
+ * The cache of B users, H heads and N rows a head (N a multiple of SOLAR_CACHE_BLOCK = 64):
+ *   k8, v8            [B,H,N,d]    e4m3
+ *   k_scale, v_scale  [B,H,N/64]   f32   one scale per block of 64 rows: a row is its bytes times the scale of its block
+ * The append writes powers of two: the smallest 2^e, e >= -100, with max|x| <= 448 * 2^e over the block's rows.
+ * Rows that were never written are never read as numbers; the cache needs no initial value.
+ *
+ * solar_history_cache_append: rows t = 0 .. counts[b] - 1 of K, V [B,T,H,d] dt become rows start[b] + t of user b,
+ * rounded to the nearest e4m3 (what is not finite becomes NaN).  A block that held rows before start[b] keeps
+ * them: where the new rows need a larger exponent, the older ones are rounded to it.  Rows at start[b] and behind it
+ * are overwritten or left as they were.  Rows past N are dropped, and a start outside 0 .. N-1 writes nothing.
+ *   start  [B] int (in)       counts [B] int (in), taken as 0 .. T; NULL: T
+ * The lengths are the caller's: lengths[b] = start[b] + counts[b] from then on.
+ *
+ * solar_history_cache_attention: O = softmax(scale * Q K^T) V over rows 0 .. lengths[b] - 1.
+ *   Q        [B,M,Hq,d] dt (in)   Hq a multiple of H: query head i reads cached head i / (Hq / H)
+ *   lengths  [B] int       (in)   taken as 0 .. N
+ *   flags                  (in)   SOLAR_FLAG_CAUSAL: the M queries are the last M rows, query m sees rows
+ *                                 0 .. lengths[b] - M + m
+ *   O        [B,M,Hq,d] dt (out)  zeros for a query that sees no row
+ * A query that sees a row of K or V that is not finite comes out NaN (in the components of that row of V at least);
+ * what it does not see does not reach it.
+ *
+ * Token tensors have strides as in solar_linear_attention_fwd.  One launch each, no workspace; results are
+ * reproducible bit for bit.  Sums and the softmax's statistics are fp32; the weights of the softmax enter their
+ * product with V as fp16 of 2^15 times their value relative to the largest (fp32 storage: two fp16 halves).
+ * H <= 21845; N <= 2^30.
+ * ------------------------------------------------------------------------- */
+#define SOLAR_CACHE_BLOCK 64
+enum { SOLAR_FLAG_CAUSAL = 2 };
+
+solar_status_t solar_history_cache_append(int B, int T, int H, int N, int d, solar_dtype_t dt,
+                                          const void* K, const long long* k_strides,
+                                          const void* V, const long long* v_strides,
+                                          const int* start, const int* counts, void* k8, void* v8,
+                                          float* k_scale, float* v_scale, void* stream);
+
+solar_status_t solar_history_cache_attention(int B, int M, int Hq, int H, int N, int d, solar_dtype_t dt,
+                                             const void* Q, const long long* q_strides,
+                                             const void* k8, const void* v8, const float* k_scale,
+                                             const float* v_scale, const int* lengths, float scale,
+                                             unsigned flags, void* O, const long long* o_strides, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

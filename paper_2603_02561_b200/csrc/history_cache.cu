@@ -1,0 +1,520 @@
+// A user's history in 8 bits, and softmax attention over it.
+//
+// The cache: rows K, V [B,H,capacity,d] in e4m3, and for every block of 64 rows of a head a scale that is a power of
+// two: the smallest 2^e (e >= -100) with max|x| <= 448 * 2^e over the block.  e4m3 has the same relative precision
+// at every magnitude down to 2^-6, so a scale between two powers of two would gain nothing; and with whole powers a scale
+// comes out of a sum as an exact factor, and a block whose exponent grows when a later row comes in is moved to the
+// new exponent without another rounding (but for values under 2^-14 of the block's largest, which e4m3 holds as
+// fractions of 2^-9).
+//
+// history_append_kernel: a CTA per block of the cache that the new rows touch, head and K or V.
+//
+// history_attention_kernel: o = softmax(scale q K^T) V over the rows that a user has, for 16 (query, head of the
+// group) rows per CTA, so that the query heads of a cached head share its rows.  Warps take blocks of 64 rows in
+// turn, each with its own running maximum and sum, and add up at the end; where the queries alone do not fill the
+// GPU, the rows are split over the CTAs of a cluster, which add up through distributed shared memory: one launch, no
+// workspace.  Rows go from global memory to registers as 8-bit fragments: a lane takes 16 bytes of a key, and the order
+// of the products' inner index is whatever those bytes are (queries are laid out to match); of the values it takes
+// the bytes of two rows that a fragment pairs, interleaved by one byte permutation.  All MMAs are fp16 x fp16 with fp32
+// sums, e4m3 being exact in fp16:
+//   q    each row by a power of two to below 2, then fp16 (bf16 storage: exact down to 2^-14 of the row's largest) or a
+//        high and a low fp16 half (fp32 storage: 22 bits)
+//   p    2^(s - m + 15), so that fp16 holds weights down to 2^-39 of the largest; fp32 storage: high and low halves
+// The sums of a block's p V are fp32 and are scaled by the block's 2^e as they join the row's.
+#include <cuda_fp16.h>
+
+#include "sm100_ptx.cuh"
+#include "solar_internal.cuh"
+
+namespace solar {
+namespace {
+
+constexpr int kBlock = SOLAR_CACHE_BLOCK;          // rows that share a scale
+constexpr int kMinExp = -100, kMaxExp = 120;       // of a scale: 448 * 2^120 is the last value below 2^129
+
+__device__ __forceinline__ float two_to(int e) { return __int_as_float((e + 127) << 23); }   // -126 <= e <= 127
+__device__ __forceinline__ int exponent_of(float x) { return (int)((__float_as_uint(x) >> 23) & 0xffu) - 127; }
+// Two floats to e4m3, nearest even; what is not finite becomes NaN.
+__device__ __forceinline__ uint32_t to_e4m3x2(float a, float b) {
+  const float nan = __int_as_float(0x7fffffff);
+  a = fabsf(a) == INFINITY ? nan : a;
+  b = fabsf(b) == INFINITY ? nan : b;
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
+  return r;
+}
+__device__ __forceinline__ uint32_t e4m3x2_to_half2(uint32_t two) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)two));
+  return r;
+}
+
+// ---- append -------------------------------------------------------------------------------------------
+template <typename T, int D>
+__global__ void __launch_bounds__(D == 32 ? 128 : 256)
+history_append_kernel(LinearOperand k, LinearOperand v, int T_new, int N, const int* start, const int* counts,
+                      uint8_t* k8, uint8_t* v8, float* k_scale, float* v_scale) {
+  constexpr int NT = D == 32 ? 128 : 256, PIECES = D / 16, CH = kBlock * PIECES / NT;
+  __shared__ float top[NT / 32];
+  const int tid = threadIdx.x, H = gridDim.y >> 1, h = blockIdx.y >> 1, b = blockIdx.z;
+  const bool value = blockIdx.y & 1;
+  pdl_wait();
+  const int first = ld_dep(start + b);
+  int n = T_new;
+  if (counts != nullptr) n = min(max(ld_dep(counts + b), 0), T_new);
+  if (first < 0 || first >= N) return;
+  const int end = min((long long)first + n, (long long)N);       // rows past the capacity are dropped
+  const int blk = first / kBlock + blockIdx.x;
+  if (blk * (long long)kBlock >= end) return;
+  const LinearOperand& src = value ? v : k;
+  const T* rows = static_cast<const T*>(src.p) + (long long)b * src.sb + (long long)h * src.sh;
+  uint8_t* cache = (value ? v8 : k8) + (((size_t)b * H + h) * N + (size_t)blk * kBlock) * D;
+  float* scale = (value ? v_scale : k_scale) + ((size_t)b * H + h) * (N / kBlock) + blk;
+  const int lo = max(first - blk * kBlock, 0), hi = min(end - blk * kBlock, kBlock);      // the new rows of this block
+  const float before = lo > 0 ? ld_dep(scale) : 0.f;
+
+  float x[CH][16], m = 0.f;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int i = tid + c * NT, row = i / PIECES, piece = i % PIECES;
+    if (row >= lo && row < hi) {
+      const T* p = rows + (long long)(blk * kBlock + row - first) * src.st + piece * 16;
+#pragma unroll
+      for (int e = 0; e < 16; e += Vec16<T>::kElems) Vec16<T>::load(p + e, &x[c][e]);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) m = fmaxf(m, fabsf(x[c][e]) < INFINITY ? fabsf(x[c][e]) : 0.f);
+    }
+  }
+#pragma unroll
+  for (int s = 16; s > 0; s >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, s));
+  if ((tid & 31) == 0) top[tid >> 5] = m;
+  __syncthreads();                                                // (and every thread has read the old scale)
+#pragma unroll
+  for (int w = 0; w < NT / 32; ++w) m = fmaxf(m, top[w]);
+  // 448 = 1.75 * 2^8
+  int e = exponent_of(m) - 8 + ((__float_as_uint(m) & 0x7fffffu) > 0x600000u ? 1 : 0);
+  e = max(e, kMinExp);
+  const int e_old = lo > 0 ? min(max(exponent_of(before), kMinExp), kMaxExp) : e;
+  e = max(e, e_old);
+  const float inv = two_to(-e);
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int i = tid + c * NT, row = i / PIECES, piece = i % PIECES;
+    uint4* at = reinterpret_cast<uint4*>(cache + row * D + piece * 16);
+    uint32_t w[4];
+    if (row >= lo && row < hi) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        w[q] = to_e4m3x2(x[c][4 * q] * inv, x[c][4 * q + 1] * inv) | (to_e4m3x2(x[c][4 * q + 2] * inv, x[c][4 * q + 3] * inv) << 16);
+      *at = make_uint4(w[0], w[1], w[2], w[3]);
+    } else if (row < lo && e > e_old) {                           // older rows of the block, to the new exponent
+      const float f = two_to(max(e_old - e, -126));
+      const uint4 o = ld_dep(at);
+      const uint32_t u[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint32_t a = e4m3x2_to_half2(u[q] & 0xffffu), d = e4m3x2_to_half2(u[q] >> 16);
+        const float2 fa = __half22float2(*reinterpret_cast<const __half2*>(&a)), fd = __half22float2(*reinterpret_cast<const __half2*>(&d));
+        w[q] = to_e4m3x2(fa.x * f, fa.y * f) | (to_e4m3x2(fd.x * f, fd.y * f) << 16);
+      }
+      *at = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+  if (tid == 0 && (lo == 0 || e > e_old)) *scale = two_to(e);
+}
+
+// ---- attention ----------------------------------------------------------------------------------------
+__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_half(float a, float b) {
+  const __half2 v = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+// (a, b) as NP pairs of fp16 whose sums are a and b
+template <int NP> __device__ __forceinline__ void split_half(float a, float b, uint32_t (&w)[NP]) {
+  w[0] = pack_half(a, b);
+  if constexpr (NP == 2) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[0]));
+    w[1] = pack_half(a - f.x, b - f.y);
+  }
+}
+
+constexpr int kRowsPerCta = 16, kWarps = 4, kMaxSplits8 = 8;
+// CTAs that an SM is to hold, by registers
+template <typename T, int D> constexpr int kPerSm = D == 128 ? 2 : D == 64 || sizeof(T) == 4 ? 3 : 4;
+constexpr float kLift = 15.f;                      // log2 of the largest weight as fp16 holds it
+
+template <int D> struct HistShared {
+  float o[kWarps][kRowsPerCta][D];                 // the warps' sums; the first is the CTA's after they have joined
+  float m[kWarps][kRowsPerCta], l[kWarps][kRowsPerCta];
+};
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kWarps * 32, kPerSm<T, D>)
+history_attention_kernel(LinearOperand q, T* O, long long ob, long long ot, long long oh, int M, int G, int N, int splits,
+                         const uint8_t* k8, const uint8_t* v8, const float* k_scale, const float* v_scale,
+                         const int* lengths, float scale, int causal) {
+  constexpr int NP = sizeof(T) == 2 ? 1 : 2;       // fp16 terms of q and p
+  constexpr int KS = D / 16, HALF = D < 64 ? D : 64, HALVES = D / HALF, NI = HALF / 8, KW = D < 64 ? 2 : 4;
+  constexpr int KC = D < 64 ? 1 : D / 64;          // loads of a key: 8 or 16 bytes a lane
+  extern __shared__ __align__(16) uint8_t smem[];
+  HistShared<D>& sh = *reinterpret_cast<HistShared<D>*>(smem);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, j = lane & 3;
+  const int rt = blockIdx.x / splits, split = blockIdx.x % splits, hk = blockIdx.y, b = blockIdx.z, H = gridDim.y;
+  const long long rows = (long long)M * G;
+
+  pdl_wait();
+  const int len = min(max(ld_dep(lengths + b), 0), N);
+  // the row of lane group g, and the one eight below: queries r / G, head r % G of the group
+  long long row[2];
+  int limit[2];                                    // cached rows that it sees
+  uint32_t qa[NP][KS][4];
+  float qs[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    row[i] = (long long)rt * kRowsPerCta + g + 8 * i;
+    const bool real = row[i] < rows;
+    const long long mq = real ? row[i] / G : 0;
+    const int hq = real ? (int)(row[i] - mq * G) : 0;
+    limit[i] = real && causal ? (int)max(min((long long)len, len - M + mq + 1), 0ll) : len;
+    const T* p = static_cast<const T*>(q.p) + (long long)b * q.sb + mq * q.st + (long long)(hk * G + hq) * q.sh;
+    float x[KS][4], top = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) {
+      const int at = D < 64 ? j * 8 + kk * 4 : (kk / 4) * 64 + j * 16 + (kk % 4) * 4;
+      if constexpr (sizeof(T) == 2) {
+        const uint2 w = ld_dep(reinterpret_cast<const uint2*>(p + at));
+        x[kk][0] = __uint_as_float(w.x << 16); x[kk][1] = __uint_as_float(w.x & 0xffff0000u);
+        x[kk][2] = __uint_as_float(w.y << 16); x[kk][3] = __uint_as_float(w.y & 0xffff0000u);
+      } else {
+        const float4 w = ld_dep(reinterpret_cast<const float4*>(p + at));
+        x[kk][0] = w.x; x[kk][1] = w.y; x[kk][2] = w.z; x[kk][3] = w.w;
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(x[kk][e]));
+    }
+    top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
+    top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
+    const int e = min(max(exponent_of(top), -126), 126);
+    const float f = two_to(-e);
+    qs[i] = scale * 1.4426950408889634f * two_to(e);
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) {
+      uint32_t a[NP], c[NP];
+      split_half<NP>(x[kk][0] * f, x[kk][1] * f, a);
+      split_half<NP>(x[kk][2] * f, x[kk][3] * f, c);
+#pragma unroll
+      for (int t = 0; t < NP; ++t) { qa[t][kk][i] = a[t]; qa[t][kk][2 + i] = c[t]; }
+    }
+  }
+  // blocks of the cache that the tile's last row reaches, this CTA's share of them
+  int reach = len;
+  if (causal) {
+    const long long last = min((long long)(rt + 1) * kRowsPerCta, rows) - 1;
+    reach = (int)max(min((long long)len, len - M + last / G + 1), 0ll);
+  }
+  const int blocks = (reach + kBlock - 1) / kBlock, per = (blocks + splits - 1) / splits;
+  const int b0 = min(split * per, blocks), b1 = min(b0 + per, blocks);
+  const uint8_t* kc = k8 + ((size_t)b * H + hk) * N * D;
+  const uint8_t* vc = v8 + ((size_t)b * H + hk) * N * D;
+  const float* ksc = k_scale + ((size_t)b * H + hk) * (N / kBlock);
+  const float* vsc = v_scale + ((size_t)b * H + hk) * (N / kBlock);
+
+  float o[HALVES][NI][4], m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
+#pragma unroll
+  for (int x = 0; x < HALVES; ++x)
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[x][i][e] = 0.f;
+
+  for (int blk = b0 + warp; blk < b1; blk += kWarps) {
+    const uint8_t* kp = kc + (size_t)blk * kBlock * D;
+    const uint8_t* vp = vc + (size_t)blk * kBlock * D;
+    const float ks = ld_dep(ksc + blk), vs = ld_dep(vsc + blk);
+    const int left = len - blk * kBlock;           // rows of the block that exist
+    float s[8][4];
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
+      uint32_t w[KC * KW];
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        if constexpr (D < 64) {
+          const uint2 u = *reinterpret_cast<const uint2*>(kp + (n * 8 + g) * D + j * 8);
+          w[0] = u.x; w[1] = u.y;
+        } else {
+          const uint4 u = *reinterpret_cast<const uint4*>(kp + (n * 8 + g) * D + c * 64 + j * 16);
+          w[4 * c] = u.x; w[4 * c + 1] = u.y; w[4 * c + 2] = u.z; w[4 * c + 3] = u.w;
+        }
+      }
+#pragma unroll
+      for (int kk = 0; kk < KS; ++kk) {
+        const uint32_t y0 = e4m3x2_to_half2(w[kk] & 0xffffu), y1 = e4m3x2_to_half2(w[kk] >> 16);
+#pragma unroll
+        for (int t = 0; t < NP; ++t) mma_f16(s[n], qa[t][kk], y0, y1);
+      }
+    }
+    // scores in log2 units, masked by position (whatever lies behind the history does not count, NaN neither)
+    float top[2] = {-INFINITY, -INFINITY};
+    const float f[2] = {qs[0] * ks, qs[1] * ks};
+    const bool whole = __all_sync(~0u, (blk + 1) * kBlock <= min(limit[0], limit[1]));
+#pragma unroll
+    for (int n = 0; n < 8; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float x = s[n][e] * f[e >> 1];
+        if (!whole && blk * kBlock + n * 8 + 2 * j + (e & 1) >= limit[e >> 1]) x = -INFINITY;
+        s[n][e] = x;
+        top[e >> 1] = fmaxf(top[e >> 1], x);
+      }
+    float corr[2], ref[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      top[i] = fmaxf(top[i], __shfl_xor_sync(~0u, top[i], 1));
+      top[i] = fmaxf(top[i], __shfl_xor_sync(~0u, top[i], 2));
+      const float m = fmaxf(m_run[i], top[i]);
+      ref[i] = m == -INFINITY ? 0.f : m - kLift;   // a row that sees nothing yet: all its weights are 2^-inf = 0
+      corr[i] = m_run[i] == -INFINITY ? 0.f : exp2f(m_run[i] - m);
+      m_run[i] = m;
+      l_run[i] *= corr[i];
+    }
+    uint32_t pa[NP][4][4];
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+      float x[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[e] = NP == 1 ? ptx::fast_exp2(s[n][e] - ref[e >> 1]) : exp2f(s[n][e] - ref[e >> 1]);
+        l_run[e >> 1] += x[e];
+      }
+      uint32_t a[NP], c[NP];
+      split_half<NP>(x[0], x[1], a);
+      split_half<NP>(x[2], x[3], c);
+#pragma unroll
+      for (int t = 0; t < NP; ++t) { pa[t][n >> 1][2 * (n & 1)] = a[t]; pa[t][n >> 1][2 * (n & 1) + 1] = c[t]; }
+    }
+    bool odd = false;                              // a value of the block that is not finite
+#pragma unroll
+    for (int x = 0; x < HALVES; ++x) {
+      uint32_t w[4][4][HALF / 32];                 // rows 16 t + 2j, + 1, + 8, + 9; bytes g * HALF / 8 ..
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int at = t * 16 + 2 * j + (r & 1) + (r >> 1) * 8;
+          const uint8_t* p = vp + at * D + x * 64 + g * (HALF / 8);
+          if constexpr (HALF == 64) {
+            const uint2 u = at < left ? *reinterpret_cast<const uint2*>(p) : make_uint2(0, 0);
+            w[t][r][0] = u.x; w[t][r][HALF / 32 - 1] = u.y;
+          } else {
+            w[t][r][0] = at < left ? *reinterpret_cast<const uint32_t*>(p) : 0u;
+          }
+        }
+      if (!whole) {
+        // rows that only some of the tile's queries see: a NaN among them must not reach the others through 0 * NaN
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int c = 0; c < HALF / 32; ++c) {
+              const uint32_t nan = __vcmpeq4(w[t][r][c] & 0x7f7f7f7fu, 0x7f7f7f7fu);
+              odd |= nan != 0;
+              w[t][r][c] &= ~nan;
+            }
+      }
+#pragma unroll
+      for (int i = 0; i < NI; i += 2) {
+        float c0[4] = {0.f, 0.f, 0.f, 0.f}, c1[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const uint32_t sel = (i & 2) ? 0x7362u : 0x5140u;
+          const uint32_t u = __byte_perm(w[t][0][i >> 2], w[t][1][i >> 2], sel), v = __byte_perm(w[t][2][i >> 2], w[t][3][i >> 2], sel);
+          const uint32_t y0 = e4m3x2_to_half2(u & 0xffffu), y1 = e4m3x2_to_half2(v & 0xffffu);
+          const uint32_t z0 = e4m3x2_to_half2(u >> 16), z1 = e4m3x2_to_half2(v >> 16);
+#pragma unroll
+          for (int n = 0; n < NP; ++n) { mma_f16(c0, pa[n][t], y0, y1); mma_f16(c1, pa[n][t], z0, z1); }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          o[x][i][e] = fmaf(o[x][i][e], corr[e >> 1], vs * c0[e]);
+          o[x][i + 1][e] = fmaf(o[x][i + 1][e], corr[e >> 1], vs * c1[e]);
+        }
+      }
+    }
+    if (__any_sync(~0u, odd)) {
+      for (int at = 0; at < min(left, kBlock); ++at)
+#pragma unroll
+        for (int x = 0; x < HALVES; ++x)
+#pragma unroll
+          for (int i = 0; i < NI; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (blk * kBlock + at < limit[e >> 1] && (vp[at * D + x * 64 + (2 * j + (e & 1)) * (HALF / 8) + i] & 0x7f) == 0x7f)
+                o[x][i][e] = __int_as_float(0x7fffffff);
+    }
+  }
+
+  // ---- the warps' sums -----------------------------------------------------------------------------------
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    l_run[i] += __shfl_xor_sync(~0u, l_run[i], 1);
+    l_run[i] += __shfl_xor_sync(~0u, l_run[i], 2);
+    if (j == 0) { sh.m[warp][g + 8 * i] = m_run[i]; sh.l[warp][g + 8 * i] = l_run[i]; }
+  }
+#pragma unroll
+  for (int x = 0; x < HALVES; ++x)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int i = 0; i < NI; i += 4)
+        *reinterpret_cast<float4*>(&sh.o[warp][g + 8 * (e >> 1)][x * 64 + (2 * j + (e & 1)) * (HALF / 8) + i]) =
+            make_float4(o[x][i][e], o[x][i + 1][e], o[x][i + 2][e], o[x][i + 3][e]);
+  __syncthreads();
+  constexpr int QUADS = kRowsPerCta * D / 4;
+  auto weight = [](float m, float top) { return m == -INFINITY ? 0.f : exp2f(m - top); };
+  if (splits > 1) {
+    float4 acc[QUADS / (kWarps * 32)];
+    float mm = 0.f, ll = 0.f;
+#pragma unroll
+    for (int c = 0; c < QUADS / (kWarps * 32); ++c) {
+      const int at = tid + c * kWarps * 32, r = at / (D / 4), piece = at % (D / 4);
+      float top = sh.m[0][r];
+#pragma unroll
+      for (int w = 1; w < kWarps; ++w) top = fmaxf(top, sh.m[w][r]);
+      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float f = weight(sh.m[w][r], top);
+        const float4 y = *reinterpret_cast<const float4*>(&sh.o[w][r][piece * 4]);
+        a.x = fmaf(f, y.x, a.x); a.y = fmaf(f, y.y, a.y); a.z = fmaf(f, y.z, a.z); a.w = fmaf(f, y.w, a.w);
+      }
+      acc[c] = a;
+    }
+    if (tid < kRowsPerCta) {
+      mm = sh.m[0][tid];
+#pragma unroll
+      for (int w = 1; w < kWarps; ++w) mm = fmaxf(mm, sh.m[w][tid]);
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) ll = fmaf(weight(sh.m[w][tid], mm), sh.l[w][tid], ll);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < QUADS / (kWarps * 32); ++c) {
+      const int at = tid + c * kWarps * 32;
+      *reinterpret_cast<float4*>(&sh.o[0][at / (D / 4)][(at % (D / 4)) * 4]) = acc[c];
+    }
+    // m and l of a row side by side where one 16-byte load brings both
+    if (tid < kRowsPerCta) *reinterpret_cast<float4*>(&sh.o[1][0][0] + 4 * tid) = make_float4(mm, ll, 0.f, 0.f);
+    ptx::cluster_sync();
+  }
+  // ---- the splits' sums, a share of the tile's outputs per CTA; then the quotient ---------------------------
+  const int sets = splits > 1 ? splits : kWarps;
+  for (int at = tid + split * kWarps * 32; at < QUADS; at += splits * kWarps * 32) {
+    const int r = at / (D / 4), piece = at % (D / 4);
+    float top = -INFINITY, l = 0.f;
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+    float ms[kMaxSplits8], ls[kMaxSplits8];
+#pragma unroll
+    for (int w = 0; w < kMaxSplits8; ++w) {
+      ms[w] = -INFINITY; ls[w] = 0.f;
+      if (w < sets) {
+        if (splits > 1) {
+          const float4 y = ptx::ld_cluster_f4(&sh.o[1][0][0] + 4 * r, w);
+          ms[w] = y.x; ls[w] = y.y;
+        } else {
+          ms[w] = sh.m[w & (kWarps - 1)][r]; ls[w] = sh.l[w & (kWarps - 1)][r];
+        }
+      }
+      top = fmaxf(top, ms[w]);
+    }
+#pragma unroll
+    for (int w = 0; w < kMaxSplits8; ++w) {
+      if (w >= sets) break;
+      const float f = weight(ms[w], top);
+      const float4 y = splits > 1 ? ptx::ld_cluster_f4(&sh.o[0][r][piece * 4], w) : *reinterpret_cast<const float4*>(&sh.o[w & (kWarps - 1)][r][piece * 4]);
+      l = fmaf(f, ls[w], l);
+      a.x = fmaf(f, y.x, a.x); a.y = fmaf(f, y.y, a.y); a.z = fmaf(f, y.z, a.z); a.w = fmaf(f, y.w, a.w);
+    }
+    const long long out = (long long)rt * kRowsPerCta + r;
+    if (out < rows) {
+      const long long mq = out / G;
+      T* p = O + (long long)b * ob + mq * ot + (long long)(hk * G + (int)(out - mq * G)) * oh + piece * 4;
+      // l = 0: a query that sees no row at all (a NaN in l or m is none: it goes on to the output)
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      if constexpr (sizeof(T) == 2)
+        *reinterpret_cast<uint2*>(p) = make_uint2(ptx::pack_bf16(a.x * inv, a.y * inv), ptx::pack_bf16(a.z * inv, a.w * inv));
+      else
+        *reinterpret_cast<float4*>(p) = make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
+    }
+  }
+  if (splits > 1) ptx::cluster_sync();             // nobody leaves while its sums are read
+}
+
+template <typename T, int D>
+cudaError_t launch_append_td(int B, int T_new, int H, int N, const LinearOperand& k, const LinearOperand& v, const int* start,
+                             const int* counts, uint8_t* k8, uint8_t* v8, float* k_scale, float* v_scale, cudaStream_t st) {
+  const dim3 grid((T_new + kBlock - 2) / kBlock + 1, 2 * H, B);
+  return launch_pdl(history_append_kernel<T, D>, grid, dim3(D == 32 ? 128 : 256), 0, st, k, v, T_new, N, start, counts, k8, v8, k_scale, v_scale);
+}
+
+template <typename T, int D>
+cudaError_t launch_attention_td(const HistoryCall& c, cudaStream_t st) {
+  const size_t smem = sizeof(HistShared<D>);
+  static bool limits_set[kMaxDevicesCached] = {};
+  const cudaError_t e = set_kernel_limits(reinterpret_cast<const void*>(&history_attention_kernel<T, D>), smem, limits_set);
+  if (e != cudaSuccess) return e;
+  const long long tiles = ((long long)c.M * c.G + kRowsPerCta - 1) / kRowsPerCta, ctas = tiles * c.H * c.B;
+  // the rows are split while the CTAs still run at once and each warp has a block to itself
+  int splits = 1;
+  while (splits < kMaxSplits8 && ctas * splits * 2 <= (long long)kNumSMs * kPerSm<T, D> && c.N / kBlock >= splits * 2 * kWarps) splits *= 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(tiles * splits), c.H, c.B);
+  cfg.blockDim = dim3(kWarps * 32);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = splits; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = splits > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, history_attention_kernel<T, D>, c.q, static_cast<T*>(c.o), c.ob, c.ot, c.oh, c.M, c.G, c.N, splits,
+                            c.k8, c.v8, c.k_scale, c.v_scale, c.lengths, c.scale, c.causal);
+}
+
+}  // namespace
+
+cudaError_t launch_history_append(int B, int T_new, int H, int N, int d, solar_dtype_t dt, const LinearOperand& k, const LinearOperand& v,
+                                  const int* start, const int* counts, uint8_t* k8, uint8_t* v8, float* k_scale, float* v_scale,
+                                  cudaStream_t st) {
+#define SOLAR_APPEND(TT, DD) return launch_append_td<TT, DD>(B, T_new, H, N, k, v, start, counts, k8, v8, k_scale, v_scale, st)
+  if (dt == SOLAR_BF16) {
+    if (d == 32) SOLAR_APPEND(__nv_bfloat16, 32);
+    if (d == 64) SOLAR_APPEND(__nv_bfloat16, 64);
+    SOLAR_APPEND(__nv_bfloat16, 128);
+  }
+  if (d == 32) SOLAR_APPEND(float, 32);
+  if (d == 64) SOLAR_APPEND(float, 64);
+  SOLAR_APPEND(float, 128);
+#undef SOLAR_APPEND
+}
+
+cudaError_t launch_history_attention(int d, solar_dtype_t dt, const HistoryCall& c, cudaStream_t st) {
+  if (dt == SOLAR_BF16) {
+    if (d == 32) return launch_attention_td<__nv_bfloat16, 32>(c, st);
+    if (d == 64) return launch_attention_td<__nv_bfloat16, 64>(c, st);
+    return launch_attention_td<__nv_bfloat16, 128>(c, st);
+  }
+  if (d == 32) return launch_attention_td<float, 32>(c, st);
+  if (d == 64) return launch_attention_td<float, 64>(c, st);
+  return launch_attention_td<float, 128>(c, st);
+}
+
+}  // namespace solar

@@ -116,6 +116,10 @@ solar_status_t check_linear(int B, int T, int H, int d, solar_dtype_t dt) {
   if (B > 65535 || H > 65535 / 3) return SOLAR_ERR_UNSUPPORTED;
   return SOLAR_OK;
 }
+solar_status_t check_cache(int N) {
+  if (N < 0 || N % SOLAR_CACHE_BLOCK != 0) return SOLAR_ERR_INVALID_ARG;
+  return N > (1 << 30) ? SOLAR_ERR_UNSUPPORTED : SOLAR_OK;
+}
 solar_status_t check_optional(const void* p, unsigned align) {
   return (reinterpret_cast<uintptr_t>(p) & (align - 1)) == 0 ? SOLAR_OK : SOLAR_ERR_INVALID_ARG;
 }
@@ -497,6 +501,52 @@ solar_status_t solar_linear_attention_step(int B, int H, int d, solar_dtype_t dt
   SOLAR_TRY(check_ptr(state));
   return from_cuda(launch_linear_step(B, H, d, dt, op[0], op[1], op[2], log_decay, scale, state, O, o.sb, o.sh,
                                       static_cast<cudaStream_t>(stream)));
+}
+
+solar_status_t solar_history_cache_append(int B, int T, int H, int N, int d, solar_dtype_t dt, const void* K, const long long* k_strides,
+                                          const void* V, const long long* v_strides, const int* start, const int* counts,
+                                          void* k8, void* v8, float* k_scale, float* v_scale, void* stream) {
+  SOLAR_TRY(check_linear(B, T, H, d, dt));
+  SOLAR_TRY(check_cache(N));
+  if (B == 0 || T == 0 || N == 0) return SOLAR_OK;
+  LinearOperand k, v;
+  SOLAR_TRY(token_input(B, T, H, d, dt, K, k_strides, &k));
+  SOLAR_TRY(token_input(B, T, H, d, dt, V, v_strides, &v));
+  SOLAR_TRY(check_word_ptr(start));
+  SOLAR_TRY(check_optional(counts, 4));
+  SOLAR_TRY(check_ptr(k8));
+  SOLAR_TRY(check_ptr(v8));
+  SOLAR_TRY(check_word_ptr(k_scale));
+  SOLAR_TRY(check_word_ptr(v_scale));
+  return from_cuda(launch_history_append(B, T, H, N, d, dt, k, v, start, counts, static_cast<uint8_t*>(k8), static_cast<uint8_t*>(v8),
+                                         k_scale, v_scale, static_cast<cudaStream_t>(stream)));
+}
+
+solar_status_t solar_history_cache_attention(int B, int M, int Hq, int H, int N, int d, solar_dtype_t dt, const void* Q,
+                                             const long long* q_strides, const void* k8, const void* v8, const float* k_scale,
+                                             const float* v_scale, const int* lengths, float scale, unsigned flags, void* O,
+                                             const long long* o_strides, void* stream) {
+  SOLAR_TRY(check_linear(B, M, H, d, dt));
+  SOLAR_TRY(check_cache(N));
+  if (flags & ~(unsigned)SOLAR_FLAG_CAUSAL) return SOLAR_ERR_UNSUPPORTED;
+  if (Hq < 1 || Hq % H != 0) return SOLAR_ERR_INVALID_ARG;
+  if (B == 0 || M == 0) return SOLAR_OK;
+  HistoryCall c = {};
+  Tokens o;
+  SOLAR_TRY(token_input(B, M, Hq, d, dt, Q, q_strides, &c.q));
+  SOLAR_TRY(token_output(B, M, Hq, d, dt, O, o_strides, &o));
+  if (N > 0) {
+    SOLAR_TRY(check_ptr(k8));
+    SOLAR_TRY(check_ptr(v8));
+    SOLAR_TRY(check_word_ptr(k_scale));
+    SOLAR_TRY(check_word_ptr(v_scale));
+  }
+  SOLAR_TRY(check_word_ptr(lengths));
+  c.B = B; c.M = M; c.H = H; c.G = Hq / H; c.N = N;
+  c.o = O; c.ob = o.sb; c.ot = o.st; c.oh = o.sh;
+  c.k8 = static_cast<const uint8_t*>(k8); c.v8 = static_cast<const uint8_t*>(v8); c.k_scale = k_scale; c.v_scale = v_scale;
+  c.lengths = lengths; c.scale = scale; c.causal = (flags & SOLAR_FLAG_CAUSAL) != 0;
+  return from_cuda(launch_history_attention(d, dt, c, static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -281,6 +281,24 @@ cudaError_t launch_linear_step(int B, int H, int d, solar_dtype_t dt, const Line
                                const LinearOperand& v, const float* log_decay, float scale, float* state, void* o,
                                long long ob, long long oh, cudaStream_t st);
 
+// The 8-bit history cache (csrc/history_cache.cu): rows [B,H,N,d] e4m3, scales [B,H,N/64].
+cudaError_t launch_history_append(int B, int T_new, int H, int N, int d, solar_dtype_t dt, const LinearOperand& k, const LinearOperand& v,
+                                  const int* start, const int* counts, uint8_t* k8, uint8_t* v8, float* k_scale, float* v_scale,
+                                  cudaStream_t st);
+// M queries of H * G heads over H cached heads.
+struct HistoryCall {
+  int B, M, H, G, N;
+  LinearOperand q;
+  void* o;
+  long long ob, ot, oh;
+  const uint8_t *k8, *v8;
+  const float *k_scale, *v_scale;
+  const int* lengths;
+  float scale;
+  int causal;
+};
+cudaError_t launch_history_attention(int d, solar_dtype_t dt, const HistoryCall& c, cudaStream_t st);
+
 // ---- per-kernel launch limits -----------------------------------------------------------------
 // Raises a kernel's dynamic shared-memory limit and asks for the largest shared-memory carve-out
 // (an SM keeps ONE carve-out at a time: kernels of several requests share an SM only if they

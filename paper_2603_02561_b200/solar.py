@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -16,7 +17,8 @@ LIB_PATH = os.path.join(_HERE, "libsolar_b200.so")
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA = range(5)
 F32, BF16 = 0, 1
-FLAG_NO_SOFTMAX = 1
+FLAG_NO_SOFTMAX, FLAG_CAUSAL = 1, 2
+CACHE_BLOCK = 64
 INFO_NOT_CONVERGED, INFO_NONFINITE, INFO_NOT_CERTIFIED, INFO_DEVICE_WAIT = 1, 2, 4, 8
 ROUTE_AUTO, ROUTE_SUBSPACE, ROUTE_FULL, ROUTE_TRIDIAG = 0, 1, 2, 3
 
@@ -60,6 +62,8 @@ SIGNATURES = {
     "solar_linear_attention_fwd": (_c_int, [_c_int] * 4 + [_c_int] + [_c_vp] * 6 + [_c_vp, _c_float] + [_c_vp] * 6),
     "solar_linear_attention_bwd": (_c_int, [_c_int] * 4 + [_c_int] + [_c_vp] * 6 + [_c_vp, _c_float] + [_c_vp] * 13),
     "solar_linear_attention_step": (_c_int, [_c_int] * 3 + [_c_int] + [_c_vp] * 6 + [_c_vp, _c_float] + [_c_vp] * 4),
+    "solar_history_cache_append": (_c_int, [_c_int] * 5 + [_c_int] + [_c_vp] * 11),
+    "solar_history_cache_attention": (_c_int, [_c_int] * 6 + [_c_int] + [_c_vp] * 7 + [_c_float, _c_uint] + [_c_vp] * 3),
 }
 
 _lib = None
@@ -519,4 +523,69 @@ def linear_attention_step(q, k, v, log_decay, scale, state, O=None, stream=None)
         state.data_ptr(), O.data_ptr(), so, _stream_on(dev, stream))
     if st:
         _check(st, "solar_linear_attention_step")
+    return O
+
+
+# ---- a history in 8 bits ---------------------------------------------------------------------------
+class HistoryCache(NamedTuple):
+    """The cache of B users: k, v [B,H,N,d] float8_e4m3fn and the scales [B,H,N/64] fp32 of their blocks of 64 rows."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+
+def history_cache(B, H, N, d, device="cuda") -> HistoryCache:
+    """An empty cache; N (rows per user and head) is rounded up to whole blocks."""
+    N = -(-N // CACHE_BLOCK) * CACHE_BLOCK
+    rows = [_empty((B, H, N, d), dtype=torch.float8_e4m3fn, device=device) for _ in range(2)]
+    return HistoryCache(*rows, *(torch.zeros((B, H, N // CACHE_BLOCK), dtype=_F32, device=device) for _ in range(2)))
+
+
+def _need_cache(cache, device):
+    k, v, ks, vs = cache
+    B, H, N, d = k.shape
+    blocks = (B, H, N // CACHE_BLOCK)
+    for t, n, shape, dtype in ((k, "k", k.shape, torch.float8_e4m3fn), (v, "v", k.shape, torch.float8_e4m3fn), (ks, "k_scale", blocks, _F32),
+                               (vs, "v_scale", blocks, _F32)):
+        _need_on(t, shape, dtype, "cache." + n, device)
+    return B, H, N, d
+
+
+def history_cache_append(k, v, cache, start, counts=None, stream=None):
+    """solar_history_cache_append: rows k, v [B,T,H,d] into `cache` from row start[b] on (the first counts[b] of them)."""
+    dt, dev, shape = k.dtype, k.device, k.shape
+    B, H, N, d = _need_cache(cache, dev)
+    T = shape[1]
+    if tuple(shape) != (B, T, H, d):
+        raise ValueError(f"k: want {(B, T, H, d)} for this cache, got {tuple(shape)}")
+    sk, sv = _strides(k, "k", shape, dt, dev), _strides(v, "v", shape, dt, dev)
+    _need_on(start, (B,), _I32, "start", dev)
+    if counts is not None:
+        _need_on(counts, (B,), _I32, "counts", dev)
+    st = (_lib or lib()).solar_history_cache_append(
+        B, T, H, N, d, dtype_code(dt), k.data_ptr(), sk, v.data_ptr(), sv, start.data_ptr(), _ptr(counts), cache[0].data_ptr(),
+        cache[1].data_ptr(), cache[2].data_ptr(), cache[3].data_ptr(), _stream_on(dev, stream))
+    if st:
+        _check(st, "solar_history_cache_append")
+
+
+def history_cache_attention(q, cache, lengths, scale, flags=0, O=None, stream=None):
+    """solar_history_cache_attention: q [B,M,Hq,d] over the first lengths[b] rows of `cache` -> O [B,M,Hq,d].
+    FLAG_CAUSAL: the queries are the last M rows."""
+    dt, dev, shape = q.dtype, q.device, q.shape
+    B, H, N, d = _need_cache(cache, dev)
+    M, Hq = shape[1], shape[2]
+    if tuple(shape) != (B, M, Hq, d):
+        raise ValueError(f"q: want {(B, M, Hq, d)} for this cache, got {tuple(shape)}")
+    sq = _strides(q, "q", shape, dt, dev)
+    _need_on(lengths, (B,), _I32, "lengths", dev)
+    if O is None:
+        O = _tokens_like(q)
+    so = _strides(O, "O", shape, dt, dev)
+    st = (_lib or lib()).solar_history_cache_attention(
+        B, M, Hq, H, N, d, dtype_code(dt), q.data_ptr(), sq, cache[0].data_ptr(), cache[1].data_ptr(), cache[2].data_ptr(),
+        cache[3].data_ptr(), lengths.data_ptr(), float(scale), int(flags), O.data_ptr(), so, _stream_on(dev, stream))
+    if st:
+        _check(st, "solar_history_cache_attention")
     return O
