@@ -382,7 +382,8 @@ solar_status_t solar_lowrank_factor_static(int B, int M, int N, int d, int r, so
  *
  * One launch, no workspace; sums run in a fixed order, so results are reproducible bit for bit.  States and sums are
  * fp32.  bf16 storage: the decayed scores and the state as an operand of q S are rounded to bf16 (the returned state is not).
- * Inputs that are not finite make the outputs of their user and head NaN from there on.
+ * An input that is not finite makes the outputs of its user and head infinite or NaN from there on, and can do so for
+ * up to 15 events before it.
  * H <= 21845; T = 0 copies state0 to state.
  * ------------------------------------------------------------------------- */
 solar_status_t solar_linear_attention_fwd(int B, int T, int H, int d, solar_dtype_t dt,
