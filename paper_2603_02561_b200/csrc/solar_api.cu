@@ -546,6 +546,7 @@ solar_status_t solar_history_cache_attention(int B, int M, int Hq, int H, int N,
   c.o = O; c.ob = o.sb; c.ot = o.st; c.oh = o.sh;
   c.k8 = static_cast<const uint8_t*>(k8); c.v8 = static_cast<const uint8_t*>(v8); c.k_scale = k_scale; c.v_scale = v_scale;
   c.lengths = lengths; c.scale = scale; c.causal = (flags & SOLAR_FLAG_CAUSAL) != 0;
+  if (history_flash_supported(d, dt, c)) return from_cuda(launch_history_flash(d, c, static_cast<cudaStream_t>(stream)));
   return from_cuda(launch_history_attention(d, dt, c, static_cast<cudaStream_t>(stream)));
 }
 

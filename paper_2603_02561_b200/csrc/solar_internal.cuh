@@ -298,6 +298,9 @@ struct HistoryCall {
   int causal;
 };
 cudaError_t launch_history_attention(int d, solar_dtype_t dt, const HistoryCall& c, cudaStream_t st);
+// The same for many queries on tcgen05 (csrc/history_flash.cu).
+bool history_flash_supported(int d, solar_dtype_t dt, const HistoryCall& c);
+cudaError_t launch_history_flash(int d, const HistoryCall& c, cudaStream_t st);
 
 // ---- per-kernel launch limits -----------------------------------------------------------------
 // Raises a kernel's dynamic shared-memory limit and asks for the largest shared-memory carve-out
