@@ -3,16 +3,16 @@
 // A CTA takes 256 (query, head of the group) rows of one cached head in two groups of 128, and walks through the cache in
 // tiles of 128 rows (d = 64) or 64 rows (d = 128: tensor memory holds scores, weights and sums of both groups).
 //   warps 0-7   a row per thread: the softmax
-//   warps 8-10  bring the tiles: 8-bit rows from global memory, a tile ahead in registers, to fp16 in shared memory
+//   warps 8-13  bring the tiles: 8-bit rows from global memory, a tile ahead in registers, to fp16 in shared memory
 //               (e4m3 is exact in fp16), once for both groups
-//   warp 11     issues the MMAs: S = Q K^T of a group's next tile, then Y += P V of its present one; while one group's
-//               rows are in their exponentials the other's products run
+//   warps 14,15 issue a group's MMAs: S = Q K^T of the next tile, as soon as the row warps hold the present one in
+//               registers, then Y += P V of the present one
 // Scales.  A query row is brought below 2 by a power of two and to fp16 (exact down to 2^-14 of its largest).  With
 // a = (that row's scores), z = a * (scale log2e 2^e ks) + log2 vs is the log of weight times value scale, and
-//   P = 2^(z - m + 7) as fp16,   Y = sum P v8,   l = sum 2^(z - m) / vs,   O = 2^-7 Y / l
+//   P = 2^(z - m + 3) as fp16,   Y = sum P v8,   l = sum 2^(z - m) / vs,   O = 2^-3 Y / l
 // where m is the largest z so far: P is then exact to fp16's 11 bits wherever the product of weight and value scale is
-// within 2^-21 of the row's largest, which is what the output is rounded by.  m is raised (Y and l rescaled) only when a
-// z passes it by more than 2^8, so that P stays below 2^15.
+// within 2^-17 of the row's largest (and to 2^-28 of that largest below), which is what the output is rounded by.  m is raised (Y and l rescaled) only when
+// the weights of a block add up to more than 2^15, and so before one of them is too large for fp16.
 // Where the queries alone do not fill the GPU the cache's rows are split over the CTAs of a cluster, which add up through
 // distributed shared memory.  Every wait is bounded; if one runs out the tile's output rows are written as NaN.
 #include <cuda_fp16.h>
@@ -25,10 +25,11 @@ namespace {
 
 constexpr int kBlock = SOLAR_CACHE_BLOCK;
 constexpr int kGroupRows = 128, kGroups = 2, kRows = kGroupRows * kGroups;
-constexpr int kConvWarp = 8, kConvWarps = 3, kMmaWarp = 11, kThreads = 384, kConvThreads = kConvWarps * 32;
-constexpr int kStages = 2, kMaxSplits = 8;
-constexpr float kRaise = 8.f, kLift = 7.f;
-constexpr int kErrKv = 0x41, kErrFree = 0x42, kErrS = 0x43, kErrSf = 0x44, kErrP = 0x45, kErrY = 0x46;
+constexpr int kConvWarp = 8, kConvWarps = 6, kMmaWarp = 14, kThreads = 512, kConvThreads = kConvWarps * 32;
+constexpr int kRowRegs = 176, kOtherRegs = 80;     // 256 threads each: together what the block is launched with, 512 x 128
+constexpr int kStages = 3, kMaxSplits = 8;
+constexpr float kLift = 3.f;
+constexpr int kErrKv = 0x41, kErrFree = 0x42, kErrS = 0x43, kErrSf = 0x44, kErrP = 0x45, kErrY = 0x46, kErrRaw = 0x47;
 
 template <int D> struct HfCfg {
   static constexpr int NTOK = D == 64 ? 128 : 64;               // cache rows of a tile
@@ -37,7 +38,8 @@ template <int D> struct HfCfg {
   static constexpr int Q_BYTES = kRows * D * 2, Q_BOX = kGroupRows * 128, Q_GROUP = KB * Q_BOX;
   static constexpr int BOX = NTOK * 128, OPER = KB * BOX, STAGE = 2 * OPER;
   static constexpr int MERGE = kRows * (D + 2) * 4;             // sums for the other CTAs of the cluster
-  static constexpr int TILES = Q_BYTES + kStages * STAGE;
+  static constexpr int RAW = 2 * NTOK * D;                      // the tile as it is in the cache
+  static constexpr int TILES = Q_BYTES + kStages * (STAGE + RAW);
   static constexpr size_t SMEM = (TILES > MERGE ? TILES : MERGE) + 1024;
   static constexpr int COL_S = 0, COL_P = kGroups * NTOK, COL_O = COL_P + kGroups * NTOK / 2 <= 256 ? 256 : 384;
   static constexpr int PIECES = 2 * NTOK * D / 16, PER = (PIECES + kConvThreads - 1) / kConvThreads;
@@ -64,6 +66,12 @@ __device__ __forceinline__ uint2 e4m3x4_to_half4(uint32_t w) {
   return r;
 }
 
+// An untiled copy of a multiple of 16 bytes, counted on `bar`
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(ptx::smem_u32(dst)),
+               "l"(src), "r"(bytes), "r"(ptx::smem_u32(bar)) : "memory");
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
@@ -73,8 +81,9 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sQ = base;                              // [2 groups][KB][128][128 B]
   uint8_t* sKV = base + F::Q_BYTES;                // [stages][K, V][KB][NTOK][128 B]
-  __shared__ __align__(8) uint64_t kv_full[kStages], kv_free[kStages], s_full[kGroups], s_free[kGroups], p_full[kGroups], y_done[kGroups], bar_end;
-  __shared__ float4 s_scale[kStages][NB];          // ks, log2 vs, 2^-7 / vs of a block
+  uint8_t* sRaw = sKV + kStages * F::STAGE;        // [stages][K, V][NTOK][D B]
+  __shared__ __align__(8) uint64_t raw_full[kStages], kv_full[kStages], kv_free[kStages], s_full[kGroups], s_free[kGroups], p_full[kGroups], y_done[kGroups], bar_end;
+  __shared__ float4 s_scale[kStages][NB];          // ks, log2 vs, 2^-3 / vs of a block
   __shared__ int s_odd[kStages];                   // a value that some of the tile's queries do not see is not finite
   __shared__ uint32_t s_tmem;
   __shared__ int s_err;
@@ -88,11 +97,11 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
 
   if (tid == 0) {
     s_err = 0;
-    for (int i = 0; i < kStages; ++i) { ptx::mbar_init(&kv_full[i], kConvWarps); ptx::mbar_init(&kv_free[i], 1); }
+    for (int i = 0; i < kStages; ++i) { ptx::mbar_init(&raw_full[i], 1); ptx::mbar_init(&kv_full[i], kConvWarps); ptx::mbar_init(&kv_free[i], kGroups); }
     for (int i = 0; i < kGroups; ++i) {
       ptx::mbar_init(&s_full[i], 1); ptx::mbar_init(&s_free[i], 4); ptx::mbar_init(&p_full[i], 4); ptx::mbar_init(&y_done[i], 1);
     }
-    ptx::mbar_init(&bar_end, 1);
+    ptx::mbar_init(&bar_end, kGroups);
     ptx::fence_mbar_init();
   }
   if (warp == kMmaWarp) ptx::tmem_alloc(&s_tmem, 512);
@@ -155,24 +164,34 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
   const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
   float m_ref = -INFINITY, l_run = 0.f;
 
-  if (warp >= kConvWarp && warp < kMmaWarp) {
-    // ---- the cache's rows: a tile ahead in registers, fp16 to shared memory -----------------------------------
+  if (warp >= kConvWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if (warp < kMmaWarp) {
+    // ---- the cache's rows: 8 bits by bulk copies, kStages tiles ahead, then to fp16 ------------------------------
     const int ct = tid - kConvWarp * 32;
-    uint4 w[F::PER];
-    auto fetch = [&](int t) {
-#pragma unroll
-      for (int i = 0; i < F::PER; ++i) {
-        const int piece = ct + i * kConvThreads, at = piece % (F::PIECES / 2), r = (t0 + t) * NTOK + at / (D / 16);
-        w[i] = make_uint4(0, 0, 0, 0);             // rows that do not exist: zeros, whatever the memory holds
-        if (piece < F::PIECES && r < len)
-          w[i] = ld_dep(reinterpret_cast<const uint4*>((piece < F::PIECES / 2 ? kc : vc) + (size_t)r * D) + at % (D / 16));
-      }
-    };
     const float* ksc = c.k_scale + ((size_t)b * c.H + hk) * (c.N / kBlock);
     const float* vsc = c.v_scale + ((size_t)b * c.H + hk) * (c.N / kBlock);
-    if (nt > 0) fetch(0);
+    auto copy = [&](int t) {                       // (a tile may reach past the capacity, which ends with a block)
+      const int first = (t0 + t) * NTOK;
+      const uint32_t bytes = (uint32_t)min(NTOK, c.N - first) * D;
+      ptx::mbar_arrive_expect_tx(&raw_full[t % kStages], 2 * bytes);
+      bulk_load(sRaw + (t % kStages) * F::RAW, kc + (size_t)first * D, bytes, &raw_full[t % kStages]);
+      bulk_load(sRaw + (t % kStages) * F::RAW + F::RAW / 2, vc + (size_t)first * D, bytes, &raw_full[t % kStages]);
+    };
+    float ks = 1.f, vs = 1.f;                      // scale of block ct of the tile
+    auto scales = [&](int t) {
+      const int blk = (t0 + t) * NB + ct;
+      const bool held = ct < NB && blk * kBlock < len;
+      ks = held ? ld_dep(ksc + blk) : 1.f;
+      vs = held ? ld_dep(vsc + blk) : 1.f;
+    };
+    if (ct == 0)
+      for (int t = 0; t < min(nt, kStages); ++t) copy(t);
+    if (nt > 0) scales(0);
     for (int t = 0; t < nt; ++t) {
       const int st = t % kStages, first = (t0 + t) * NTOK;
+      const uint8_t* raw = sRaw + st * F::RAW;
+      ptx::mbar_wait(&raw_full[st], (t / kStages) & 1, err, kErrRaw);
       if (t >= kStages) ptx::mbar_wait(&kv_free[st], (t / kStages - 1) & 1, err, kErrFree);
       __syncwarp();
       const bool mixed = first + NTOK > least && c.causal;      // some queries do not see all of the tile's rows
@@ -181,7 +200,9 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
       for (int i = 0; i < F::PER; ++i) {
         const int piece = ct + i * kConvThreads, at = piece % (F::PIECES / 2), r = at / (D / 16), p = at % (D / 16);
         if (piece >= F::PIECES) break;
-        uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+        uint4 w = *reinterpret_cast<const uint4*>(raw + piece * 16);
+        if (first + r >= len) w = make_uint4(0, 0, 0, 0);       // rows that do not exist: zeros, whatever the memory holds
+        uint32_t x[4] = {w.x, w.y, w.z, w.w};
         if (mixed && piece >= F::PIECES / 2) {
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
@@ -197,59 +218,56 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
       }
       if (ct == 0) s_odd[st] = 0;
       if (ct < NB) {
-        const int blk = (t0 + t) * NB + ct;
-        const bool held = blk * kBlock < len;
-        const float ks = held ? ld_dep(ksc + blk) : 1.f, vs = held ? ld_dep(vsc + blk) : 1.f;
         const float lv = vs < 1.1754944e-38f ? -126.f : log2f(vs);
         s_scale[st][ct] = make_float4(ks, lv, exp2f(-lv - kLift), 0.f);
       }
       asm volatile("bar.sync 1, %0;" ::"n"(kConvThreads) : "memory");
+      if (ct == 0 && t + kStages < nt) copy(t + kStages);       // everybody has read the tile's bytes
+      if (t + 1 < nt) scales(t + 1);
       if (odd) s_odd[st] = 1;
-      if (t + 1 < nt) fetch(t + 1);
       ptx::fence_proxy_async_smem();
       ptx::mbar_arrive_warp(&kv_full[st], lane);
     }
-  } else if (warp == kMmaWarp) {
-    if (lane == 0 && nt > 0) {
+    if (ct == 0 && *err != 0)                      // a wait ran out: the copies land before the CTA leaves
+      for (int t = max(0, nt - kStages); t < nt; ++t) {
+        int dummy = 0;
+        ptx::mbar_wait(&raw_full[t % kStages], (t / kStages) & 1, &dummy, 0);
+      }
+    } else if (lane == 0 && nt > 0) {
+      const int x = warp - kMmaWarp;
       const uint32_t idesc_s = idesc_f16(kGroupRows, NTOK, false), idesc_y = idesc_f16(kGroupRows, D, true);
-      auto scores = [&](int x, int t) {
-        const uint32_t k = ptx::smem_u32(sKV + (t % kStages) * F::STAGE), q = ptx::smem_u32(sQ + x * F::Q_GROUP);
+      const uint32_t q = ptx::smem_u32(sQ + x * F::Q_GROUP);
+      auto scores = [&](int t) {
+        const uint32_t k = ptx::smem_u32(sKV + (t % kStages) * F::STAGE);
+        if (!ptx::mbar_wait(&kv_full[t % kStages], (t / kStages) & 1, err, kErrKv)) return false;
+        ptx::tc_fence_after_sync();
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk)
           ptx::umma_bf16_ss(s_tmem + F::COL_S + x * NTOK, ptx::umma_smem_desc(q + (kk / 4) * F::Q_BOX + (kk % 4) * 32, 0, 1024),
                             ptx::umma_smem_desc(k + (kk / 4) * F::BOX + (kk % 4) * 32, 0, 1024), idesc_s, kk != 0);
         ptx::umma_commit(&s_full[x]);
+        return true;
       };
-      bool ok = ptx::mbar_wait(&kv_full[0], 0, err, kErrKv);
-      ptx::tc_fence_after_sync();
-      if (ok) { scores(0, 0); scores(1, 0); }
+      bool ok = scores(0);
       for (int t = 0; ok && t < nt; ++t) {
+        if (t + 1 < nt) ok = ptx::mbar_wait(&s_free[x], t & 1, err, kErrSf) && scores(t + 1);
+        ok = ok && ptx::mbar_wait(&p_full[x], t & 1, err, kErrP);
+        if (!ok) break;
+        ptx::tc_fence_after_sync();
         const uint32_t v = ptx::smem_u32(sKV + (t % kStages) * F::STAGE + F::OPER);
-#pragma unroll 1
-        for (int x = 0; ok && x < kGroups; ++x) {
-          if (t + 1 < nt) {
-            if (x == 0) ok = ptx::mbar_wait(&kv_full[(t + 1) % kStages], ((t + 1) / kStages) & 1, err, kErrKv);
-            ok = ok && ptx::mbar_wait(&s_free[x], t & 1, err, kErrSf);
-            if (!ok) break;
-            ptx::tc_fence_after_sync();
-            scores(x, t + 1);
-          }
-          ok = ptx::mbar_wait(&p_full[x], t & 1, err, kErrP);
-          if (!ok) break;
-          ptx::tc_fence_after_sync();
 #pragma unroll
-          for (int kk = 0; kk < NTOK / 16; ++kk)
-            // V rows are the inner index: 16 of them are two groups of 8 rows of 128 B; its columns come in blocks of 64
-            ptx::umma_bf16_ts(s_tmem + F::COL_O + x * D, s_tmem + F::COL_P + x * (NTOK / 2) + kk * 8,
-                              ptx::umma_smem_desc(v + kk * 2048, F::BOX, 1024), idesc_y, (t | kk) != 0);
-          ptx::umma_commit(&y_done[x]);
-        }
-        if (ok) ptx::umma_commit(&kv_free[t % kStages]);
+        for (int kk = 0; kk < NTOK / 16; ++kk)
+          // V rows are the inner index: 16 of them are two groups of 8 rows of 128 B; its columns come in blocks of 64
+          ptx::umma_bf16_ts(s_tmem + F::COL_O + x * D, s_tmem + F::COL_P + x * (NTOK / 2) + kk * 8,
+                            ptx::umma_smem_desc(v + kk * 2048, F::BOX, 1024), idesc_y, (t | kk) != 0);
+        ptx::umma_commit(&y_done[x]);
+        ptx::umma_commit(&kv_free[t % kStages]);
       }
       ptx::umma_commit(&bar_end);
     }
   } else {
     // ---- row warps ---------------------------------------------------------------------------------------------
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRowRegs));
     const uint32_t tm_s = s_tmem + lane_base + F::COL_S + grp * NTOK, tm_p = s_tmem + lane_base + F::COL_P + grp * (NTOK / 2),
                    tm_y = s_tmem + lane_base + F::COL_O + grp * D;
     for (int t = 0; t < nt; ++t) {
@@ -273,84 +291,95 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
       const int odd = *(volatile int*)&s_odd[st];
       ptx::tc_fence_before_sync();
       ptx::mbar_arrive_warp(&s_free[grp], lane);
-      if (first + NTOK > limit) {
+      if (__any_sync(0xffffffffu, first + NTOK > limit)) {
 #pragma unroll
         for (int j = 0; j < NTOK; ++j) s[j] = first + j < limit ? s[j] : -INFINITY;
       }
-      float f[NB], m_tile = -INFINITY;
+      float f[NB], off[NB], add;
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
-        float mx[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) mx[q] = s[n * kBlock + q];
-#pragma unroll
-        for (int j = 4; j < kBlock; j += 8)
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            mx[q] = j + 4 < kBlock ? fmaxf(fmaxf(mx[q], s[n * kBlock + j + q]), s[n * kBlock + j + 4 + q]) : fmaxf(mx[q], s[n * kBlock + j + q]);
         f[n] = qs * sc[n].x;
         f[n] = f[n] < 1.1754944e-38f ? 1.1754944e-38f : f[n];         // so that -inf stays -inf
-        m_tile = fmaxf(m_tile, fmaf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), f[n], sc[n].y));
       }
-      if (t == 0) m_ref = m_tile;
-      else if (__any_sync(0xffffffffu, m_tile > m_ref + kRaise)) {
-        // rare: once Y is up to date nobody else touches this thread's row of it
+      if (t > 0) {                                 // the weights before have been read, and Y is up to date
         ptx::mbar_wait(&y_done[grp], (t - 1) & 1, err, kErrY);
-        const float m_new = fmaxf(m_ref, m_tile), alpha = m_ref == -INFINITY ? 0.f : ptx::fast_exp2(m_ref - m_new);
-        m_ref = m_new;
-        l_run *= alpha;
         __syncwarp();
         ptx::tc_fence_after_sync();
+      }
+      // The weights, with the reference that the tiles before have left; only where a block's sum shows that one may be
+      // too large for fp16 (or there is no reference yet) is the tile's maximum looked for, and the weights made again.
+      bool look = t == 0 || __any_sync(0xffffffffu, m_ref == -INFINITY);
+#pragma unroll 1
+      for (int round = 0; round < 3; ++round) {
 #pragma unroll
-        for (int c0 = 0; c0 < D; c0 += 16) {
-          uint32_t v[16];
-          ptx::tmem_ld_32x16(tm_y + c0, v);
-          ptx::tmem_ld_wait();
+        for (int n = 0; n < NB; ++n) off[n] = sc[n].y - (m_ref == -INFINITY ? 0.f : m_ref) + kLift;
+        if (look) {
+          float m_tile = -INFINITY;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * alpha);
-          ptx::tmem_st_32x16(tm_y + c0, v);
+          for (int n = 0; n < NB; ++n) {
+            float mx[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) mx[q] = s[n * kBlock + q];
+#pragma unroll
+            for (int j = 4; j < kBlock; ++j) mx[j % 4] = fmaxf(mx[j % 4], s[n * kBlock + j]);
+            m_tile = fmaxf(m_tile, fmaf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), f[n], sc[n].y));
+          }
+          const float m_new = fmaxf(m_ref, m_tile), alpha = m_ref == -INFINITY ? 0.f : ptx::fast_exp2(m_ref - m_new);
+          m_ref = m_new;
+          l_run *= alpha;
+          if (t > 0) {
+#pragma unroll
+            for (int c0 = 0; c0 < D; c0 += 16) {
+              uint32_t v[16];
+              ptx::tmem_ld_32x16(tm_y + c0, v);
+              ptx::tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * alpha);
+              ptx::tmem_st_32x16(tm_y + c0, v);
+            }
+            ptx::tmem_st_wait();
+          }
+          const float ref = m_ref == -INFINITY ? 0.f : m_ref;
+#pragma unroll
+          for (int n = 0; n < NB; ++n) off[n] = sc[n].y - ref + kLift;
+          if (__any_sync(0xffffffffu, fabsf(ref) > 65536.f)) {
+            // scores so large that a product's rounding, which m has and the fused product below has not, is itself a factor
+#pragma unroll
+            for (int j = 0; j < NTOK; ++j) s[j] = fmaf(s[j], f[j / kBlock], sc[j / kBlock].y) - ref;
+#pragma unroll
+            for (int n = 0; n < NB; ++n) { f[n] = 1.f; off[n] = kLift; }
+          }
         }
-        ptx::tmem_st_wait();
-      }
-      const float ref = m_ref == -INFINITY ? 0.f : m_ref;
-      float off[NB];
+        add = 0.f;
+        float most = 0.f;
 #pragma unroll
-      for (int n = 0; n < NB; ++n) off[n] = sc[n].y - ref + kLift;
-      if (__any_sync(0xffffffffu, fabsf(ref) > 65536.f)) {
-        // scores so large that a product's rounding, which m has and the fused product below has not, is itself a factor
+        for (int n = 0; n < NB; ++n) {
+          float2 sum2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+          const float2 f2 = make_float2(f[n], f[n]), off2 = make_float2(off[n], off[n]);
 #pragma unroll
-        for (int j = 0; j < NTOK; ++j) s[j] = fmaf(s[j], f[j / kBlock], sc[j / kBlock].y) - ref;
+          for (int c0 = 0; c0 < kBlock; c0 += 32) {
+            uint32_t w[16];
 #pragma unroll
-        for (int n = 0; n < NB; ++n) { f[n] = 1.f; off[n] = kLift; }
-      }
-      uint32_t w[NTOK / 2];
-#pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        float2 sum2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-        const float2 f2 = make_float2(f[n], f[n]), off2 = make_float2(off[n], off[n]);
-#pragma unroll
-        for (int j = 0; j < kBlock; j += 2) {
-          const float2 x = fma2(make_float2(s[n * kBlock + j], s[n * kBlock + j + 1]), f2, off2);
-          const float2 e = make_float2(ptx::fast_exp2(x.x), ptx::fast_exp2(x.y));
-          sum2[(j / 2) % 2] = ptx::add2(sum2[(j / 2) % 2], e);
-          w[(n * kBlock + j) / 2] = half_pair(e.x, e.y);
+            for (int j = c0; j < c0 + 32; j += 2) {
+              const float2 x = fma2(make_float2(s[n * kBlock + j], s[n * kBlock + j + 1]), f2, off2);
+              const float2 e = make_float2(ptx::fast_exp2(x.x), ptx::fast_exp2(x.y));
+              sum2[(j / 2) % 2] = ptx::add2(sum2[(j / 2) % 2], e);
+              w[(j - c0) / 2] = half_pair(e.x, e.y);
+            }
+            ptx::tmem_st_32x16(tm_p + (n * kBlock + c0) / 2, w);
+          }
+          const float sum = (sum2[0].x + sum2[0].y) + (sum2[1].x + sum2[1].y);
+          most = fmaxf(most, sum);
+          add = fmaf(sum, sc[n].z, add);
         }
-        l_run = fmaf((sum2[0].x + sum2[0].y) + (sum2[1].x + sum2[1].y), sc[n].z, l_run);
+        look = __any_sync(0xffffffffu, most > 32768.f);
+        if (!look) break;
       }
+      l_run += add;
       if (odd) {                                   // a value that is not finite, for the queries that see it
         for (int j = first; j < min(limit, first + NTOK); ++j)
           for (int i = 0; i < D; ++i)
             if ((vc[(size_t)j * D + i] & 0x7f) == 0x7f) l_run = __int_as_float(0x7fffffff);
-      }
-      if (t > 0) ptx::mbar_wait(&y_done[grp], (t - 1) & 1, err, kErrY);      // the weights before have been read
-      __syncwarp();
-      ptx::tc_fence_after_sync();
-#pragma unroll
-      for (int q = 0; q < NTOK / 2; q += 16) {
-        uint32_t v[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = w[q + i];
-        ptx::tmem_st_32x16(tm_p + q, v);
       }
       ptx::tmem_st_wait();
       ptx::tc_fence_before_sync();
