@@ -26,7 +26,7 @@ namespace {
 constexpr int kBlock = SOLAR_CACHE_BLOCK;
 constexpr int kGroupRows = 128, kGroups = 2, kRows = kGroupRows * kGroups;
 constexpr int kConvWarp = 8, kConvWarps = 6, kMmaWarp = 14, kThreads = 512, kConvThreads = kConvWarps * 32;
-constexpr int kRowRegs = 176, kOtherRegs = 80;     // 256 threads each: together what the block is launched with, 512 x 128
+constexpr int kRowRegs = 192, kOtherRegs = 64;     // 256 threads each: together what the block is launched with, 512 x 128
 constexpr int kStages = 3, kMaxSplits = 8;
 constexpr float kLift = 3.f;
 constexpr int kErrKv = 0x41, kErrFree = 0x42, kErrS = 0x43, kErrSf = 0x44, kErrP = 0x45, kErrY = 0x46, kErrRaw = 0x47;
