@@ -31,7 +31,7 @@ namespace solar {
 namespace {
 
 __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -43,8 +43,11 @@ __device__ __forceinline__ void ldsm_t(uint32_t (&x)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(addr) : "memory");
 }
-// 16 bytes to shared memory, zeros where `real` is false (the address is then not read)
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool real) {
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+// zeros where `real` is false (the address is then not read)
+__device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void* src, bool real) {
   const int n = real ? 16 : 0;
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
 }
@@ -63,6 +66,11 @@ template <int NP> __device__ __forceinline__ void split(float a, float b, uint32
   }
 }
 
+// (x, y) *= f in one instruction
+__device__ __forceinline__ void mul2(float& x, float& y, float f) {
+  asm("{\n\t.reg .b64 a, b;\n\tmov.b64 a, {%0, %1};\n\tmov.b64 b, {%2, %2};\n\tmul.rn.f32x2 a, a, b;\n\tmov.b64 {%0, %1}, a;\n\t}" : "+f"(x), "+f"(y) : "f"(f));
+}
+
 template <typename T, int D> struct LaCfg {
   static constexpr int NP = sizeof(T) == 2 ? 1 : 3;            // bf16 terms of an element
   static constexpr int NA = sizeof(T) == 2 ? 2 : 3;            // of a decayed key
@@ -76,7 +84,8 @@ template <typename T, int D> struct LaCfg {
   static constexpr int SBUF = NP == 1 ? 2 : 1;                 // copies of the state as an operand
   static constexpr int STATE = NP * D * PITCH;
   static constexpr int OFF_S = STAGES * 3 * OPER, OFF_W = OFF_S + SBUF * STATE;
-  static constexpr size_t SMEM = OFF_W + (C + 1) * sizeof(float);
+  static constexpr int OFF_K = OFF_W + (C + 4) * 4;            // the keys' weights
+  static constexpr size_t SMEM = OFF_K + 2 * C * sizeof(float);
   static constexpr int PER_SM = SMEM <= 56 * 1024 ? 4 : SMEM <= 75 * 1024 ? 3 : SMEM <= 113 * 1024 ? 2 : 1;
   static_assert(STAGES * 3 * OPER >= D * D * 4, "the segments' states lie over the tiles");
 };
@@ -89,6 +98,7 @@ linear_attention_kernel(const __grid_constant__ LinearParams prm) {
   extern __shared__ __align__(16) uint8_t smem[];
   const uint32_t sbase = ptx::smem_u32(smem);
   float* sw = reinterpret_cast<float*>(smem + F::OFF_W);       // g^0 .. g^C
+  float* swk = reinterpret_cast<float*>(smem + F::OFF_K);      // what a chunk's keys enter the state with, then zeros
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, j = lane & 3;
   const int seg = blockIdx.x, segs = gridDim.x;
   const int h = blockIdx.y / prm.roles, b = blockIdx.z;
@@ -101,6 +111,7 @@ linear_attention_kernel(const __grid_constant__ LinearParams prm) {
   if (prm.lengths != nullptr) len = min(max(ld_dep(prm.lengths + b), 0), prm.T);
   auto power = [&](int n) { return n == 0 ? 1.f : exp2f((float)n * l2); };      // (0 * -inf: a head that forgets at once)
   for (int i = tid; i <= C; i += NT) sw[i] = power(i);
+  for (int i = tid; i < 2 * C; i += NT) swk[i] = i < C ? R.ak * power(C - 1 - i + rev) : 0.f;
 
   const int chunks = (len + C - 1) / C, per = (chunks + segs - 1) / segs;
   const int c0 = min(seg * per, chunks), c1 = min(c0 + per, chunks);
@@ -112,13 +123,20 @@ linear_attention_kernel(const __grid_constant__ LinearParams prm) {
   // chunk c of an operand to shared memory: rows behind the sequence are zeros
   auto load = [&](const T* p, long long st, int c, uint32_t dst) {
     if constexpr (NP == 1) {
-      constexpr int PIECES = D / 8;
+      constexpr int PIECES = D / 8, ROWS = NT / PIECES;            // rows of 16-byte pieces per turn
+      const int x0 = tid / PIECES, piece = tid % PIECES, at0 = c * C + x0;
+      const long long step = rev ? -st : st;
+      const T* from = p + (long long)(rev ? len - 1 - at0 : at0) * st + piece * 8;
+      const uint32_t to = dst + x0 * PITCH + piece * 16;
+      if ((c + 1) * C <= len) {
 #pragma unroll
-      for (int i = tid; i < C * PIECES; i += NT) {
-        const int x = i / PIECES, piece = i % PIECES, at = c * C + x;
-        const bool real = at < len;
-        const long long t = real ? (rev ? len - 1 - at : at) : 0;
-        cp_async16(dst + x * PITCH + piece * 16, p + t * st + piece * 8, real);
+        for (int i = 0; i < C / ROWS; ++i) cp_async16(to + i * ROWS * PITCH, from + i * ROWS * step);
+      } else {
+#pragma unroll
+        for (int i = 0; i < C / ROWS; ++i) {
+          const bool real = at0 + i * ROWS < len;
+          cp_async16_or_zero(to + i * ROWS * PITCH, real ? from + i * ROWS * step : p, real);
+        }
       }
     } else {
       constexpr int PIECES = D / 4;
@@ -151,17 +169,11 @@ linear_attention_kernel(const __grid_constant__ LinearParams prm) {
   auto update = [&](uint32_t sk, uint32_t sv, int n_real) {
     const float gn = sw[n_real];
 #pragma unroll
-    for (int n = 0; n < F::SC / 8; ++n)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) st[n][i] *= gn;
+    for (int n = 0; n < F::SC / 8; ++n) { mul2(st[n][0], st[n][1], gn); mul2(st[n][2], st[n][3], gn); }
+    const float* wk = swk + (C - n_real) + 2 * j;
 #pragma unroll
     for (int ks = 0; ks < C / 16; ++ks) {
-      float w[4];                                                  // of tokens 2j, 2j+1, 2j+8, 2j+9
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int s = ks * 16 + 2 * j + (i & 1) + (i >> 1) * 8;
-        w[i] = s < n_real ? R.ak * sw[n_real - 1 - s + rev] : 0.f;
-      }
+      const float w[4] = {wk[ks * 16], wk[ks * 16 + 1], wk[ks * 16 + 8], wk[ks * 16 + 9]};   // of tokens 2j, 2j+1, 2j+8, 2j+9
       uint32_t a[NA][4];
       {
         uint32_t x[NP][4];
@@ -179,18 +191,19 @@ linear_attention_kernel(const __grid_constant__ LinearParams prm) {
         }
       }
 #pragma unroll
-      for (int n2 = 0; n2 < F::SC / 16; ++n2)
+      for (int pb = 0; pb < NP; ++pb) {
+        uint32_t y[F::SC / 16][4];
 #pragma unroll
-        for (int pb = 0; pb < NP; ++pb) {
-          uint32_t y[4];
-          ldsm_t(y, sv + pb * F::TILE + ks * 16 * PITCH + (nh * F::SC + n2 * 16) * 2 + off_nm);
+        for (int n2 = 0; n2 < F::SC / 16; ++n2)
+          ldsm_t(y[n2], sv + pb * F::TILE + ks * 16 * PITCH + (nh * F::SC + n2 * 16) * 2 + off_nm);
 #pragma unroll
-          for (int pa = 0; pa < NA; ++pa)
-            if (pa + pb < NA) {
-              mma(st[2 * n2], a[pa], y[0], y[1]);
-              mma(st[2 * n2 + 1], a[pa], y[2], y[3]);
-            }
-        }
+        for (int pa = 0; pa < NA - pb; ++pa)       // (an accumulator's next product is SC / 8 products away)
+#pragma unroll
+          for (int n2 = 0; n2 < F::SC / 16; ++n2) {
+            mma(st[2 * n2], a[pa], y[n2][0], y[n2][1]);
+            mma(st[2 * n2 + 1], a[pa], y[n2][2], y[n2][3]);
+          }
+      }
     }
   };
 
@@ -266,7 +279,17 @@ linear_attention_kernel(const __grid_constant__ LinearParams prm) {
   };
 
   // ---- outputs, chunk by chunk ------------------------------------------------------------------------
-  const int rw = warp % F::RW, cw = warp / F::RW;
+  // (rows further down have more keys: the two column halves' warps of a scheduler, or the CTAs of an SM, take turns)
+  const int cw = warp / F::RW, rw0 = warp % F::RW, rw = F::CW > 1 ? (cw & 1 ? F::RW - 1 - rw0 : rw0) : (warp + seg + h) % F::RW;
+  // What this thread's eight scores of a 16 x 16 tile are multiplied by: on the diagonal (zero above it), and, but for a
+  // power of g^16, below it.
+  float near[8], far[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int gap = g + ((i >> 1) & 1) * 8 - (2 * j + (i & 1) + (i >> 2) * 8);
+    near[i] = gap >= 0 ? R.ap * power(gap) : 0.f;
+    far[i] = R.ap * power(16 + gap);
+  }
   if (c0 < c1) {
     put_state(0);
     if (NP == 1) {
@@ -320,31 +343,39 @@ linear_attention_kernel(const __grid_constant__ LinearParams prm) {
     {
       const float f0 = R.aq * sw[t0 + 1 - rev], f1 = R.aq * sw[t1 + 1 - rev];
 #pragma unroll
-      for (int n = 0; n < F::OC / 8; ++n) { o[n][0] *= f0; o[n][1] *= f0; o[n][2] *= f1; o[n][3] *= f1; }
+      for (int n = 0; n < F::OC / 8; ++n) { mul2(o[n][0], o[n][1], f0); mul2(o[n][2], o[n][3], f1); }
     }
     // scores of 16 keys at a time, decayed, times their values
 #pragma unroll
     for (int kt = 0; kt < C / 16; ++kt) {
       if (kt > rw) break;
-      float p0[4] = {0.f, 0.f, 0.f, 0.f}, p1[4] = {0.f, 0.f, 0.f, 0.f};
+      float p0[4], p1[4];
+      {
+        float z[2][2][4];                          // two chains for each half of the keys
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks)
+        for (int i = 0; i < 4; ++i) z[0][0][i] = z[0][1][i] = z[1][0][i] = z[1][1][i] = 0.f;
 #pragma unroll
-        for (int pb = 0; pb < NP; ++pb) {
-          uint32_t y[4];
-          ldsm(y, sk + pb * F::TILE + kt * 16 * PITCH + ks * 32 + off_mn);
+        for (int ks = 0; ks < D / 16; ++ks)
 #pragma unroll
-          for (int pa = 0; pa < NP; ++pa)
-            if (pa + pb < NP) {
-              mma(p0, q[pa][ks], y[0], y[1]);
-              mma(p1, q[pa][ks], y[2], y[3]);
+          for (int pb = 0; pb < NP; ++pb) {
+            uint32_t y[4];
+            ldsm(y, sk + pb * F::TILE + kt * 16 * PITCH + ks * 32 + off_mn);
+#pragma unroll
+            for (int pa = 0; pa < NP - pb; ++pa) {
+              mma(z[(ks + pa) & 1][0], q[pa][ks], y[0], y[1]);
+              mma(z[(ks + pa) & 1][1], q[pa][ks], y[2], y[3]);
             }
-        }
+          }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int t = (i >> 1) ? t1 : t0, s0 = kt * 16 + 2 * j + (i & 1), s1 = s0 + 8;
-        p0[i] = t >= s0 ? p0[i] * (R.ap * sw[t - s0]) : 0.f;
-        p1[i] = t >= s1 ? p1[i] * (R.ap * sw[t - s1]) : 0.f;
+        for (int i = 0; i < 4; ++i) { p0[i] = z[0][0][i] + z[1][0][i]; p1[i] = z[0][1][i] + z[1][1][i]; }
+      }
+      if (kt == rw) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { p0[i] *= near[i]; p1[i] *= near[4 + i]; }
+      } else {
+        const float f = sw[16 * (rw - kt - 1)];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { p0[i] *= f * far[i]; p1[i] *= f * far[4 + i]; }
       }
       uint32_t a[NP][4];
       {
@@ -417,7 +448,7 @@ template <typename F> int linear_segments(long long ctas, int T) {
   const long long slots = (long long)kNumSMs * F::PER_SM;
   long long best = -1;
   int segs = 1;
-  for (int s = 1; s <= kMaxSegments && s <= chunks; s *= 2) {
+  for (int s = 1; s <= kMaxSegments && s <= chunks; ++s) {
     const long long waves = (ctas * s + slots - 1) / slots;
     const long long per = (chunks + s - 1) / s, cost = waves * (s > 1 ? 3 * per + 4 : 2 * per);
     if (best < 0 || cost < best) { best = cost; segs = s; }
