@@ -121,13 +121,6 @@ def _stream(stream=None):
     return torch.cuda.current_stream().cuda_stream
 
 
-def _stream_on(device, stream=None):
-    """The stream of a call whose tensors are on `device`, which has to be the current one: a launch goes there."""
-    if device.index is not None and _current_device is not None and device.index != _current_device():
-        raise ValueError(f"tensors on {device}, but the current device is cuda:{_current_device()}")
-    return _stream(stream)
-
-
 def _check(status: int, where: str):
     if status != OK:
         raise SolarError(status, where)
@@ -436,48 +429,64 @@ def forward(H, C, Wq, Wk, Wv, r, scale, flags=0, workspace=None, stream=None):
 
 
 # ---- linear attention with a decay per head ------------------------------------------------------
-def _strides(t, name, shape, dtype, device):
-    """A token tensor's strides for the library: None where it is dense."""
-    if t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_cuda:
-        raise ValueError(f"{name}: want {dtype} {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+# (What these calls look at is kept to the cheapest form: `get_device()` for the device and CUDA in one, the strides of a
+# tensor that is not dense as an array made once per set of strides.)
+_stride_arrays = {}
+
+
+def _tokens(t, name, shape, dtype, dev):
+    """Looks at a token tensor; its strides for the library, None where it is dense."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
+        raise ValueError(f"{name}: want {dtype} {tuple(shape)} on cuda:{dev}, got {t.dtype} {tuple(t.shape)} on {t.device}")
     if t.is_contiguous():
         return None
-    if t.stride(-1) != 1:
-        raise ValueError(f"{name}: the last dimension has to be dense, got strides {t.stride()}")
-    return (ctypes.c_longlong * 3)(*t.stride()[:-1])
+    st = t.stride()
+    if st[-1] != 1:
+        raise ValueError(f"{name}: the last dimension has to be dense, got strides {st}")
+    arr = _stride_arrays.get(st)
+    if arr is None:
+        if len(_stride_arrays) >= 1024:
+            _stride_arrays.clear()
+        arr = _stride_arrays[st] = (ctypes.c_longlong * (len(st) - 1))(*st[:-1])
+    return arr
 
 
-def _need_on(t, shape, dtype, name, device):
-    _need(t, shape, dtype, name)
-    if t.device != device:
-        raise ValueError(f"{name}: want it on {device}, got {t.device}")
+def _dense(t, shape, dtype, name, dev):
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{name}: want contiguous {dtype} {tuple(shape)} on cuda:{dev}, got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
-def _tokens_like(t):
-    return _empty(t.shape, dtype=t.dtype, device=t.device)
+def _device_of(t, name, dims):
+    """The index of a tensor's device, which has to be the current one: a launch goes there."""
+    dev = t.get_device()
+    if dev < 0 or t.dim() != dims:
+        raise ValueError(f"{name}: want a CUDA tensor of {dims} dimensions, got {tuple(t.shape)} on {t.device}")
+    if _current_device is not None and dev != _current_device():
+        raise ValueError(f"{name}: on cuda:{dev}, but the current device is cuda:{_current_device()}")
+    return dev
 
 
 def linear_attention_fwd(q, k, v, log_decay, scale, state0=None, lengths=None, O=None, state=None, stream=None):
     """solar_linear_attention_fwd: q, k, v [B,T,H,d] (any strides with a dense last dimension) -> O [B,T,H,d] and the
     last state [B,H,d,d] fp32."""
-    B, T, H, d = q.shape
-    dt, dev, shape = q.dtype, q.device, q.shape
-    ss = [_strides(t, n, shape, dt, dev) for t, n in ((q, "q"), (k, "k"), (v, "v"))]
-    _need_on(log_decay, (H,), _F32, "log_decay", dev)
+    dt, dev, shape = q.dtype, _device_of(q, "q", 4), q.shape
+    B, T, H, d = shape
+    sq, sk, sv = _tokens(q, "q", shape, dt, dev), _tokens(k, "k", shape, dt, dev), _tokens(v, "v", shape, dt, dev)
+    _dense(log_decay, (H,), _F32, "log_decay", dev)
     if lengths is not None:
-        _need_on(lengths, (B,), _I32, "lengths", dev)
+        _dense(lengths, (B,), _I32, "lengths", dev)
     if state0 is not None:
-        _need_on(state0, (B, H, d, d), _F32, "state0", dev)
+        _dense(state0, (B, H, d, d), _F32, "state0", dev)
     if O is None:
-        O = _tokens_like(q)
-    so = _strides(O, "O", shape, dt, dev)
+        O = q.new_empty(shape)
+    so = _tokens(O, "O", shape, dt, dev)
     if state is None:
-        state = _empty((B, H, d, d), dtype=_F32, device=dev)
+        state = q.new_empty((B, H, d, d), dtype=_F32)
     else:
-        _need_on(state, (B, H, d, d), _F32, "state", dev)
+        _dense(state, (B, H, d, d), _F32, "state", dev)
     st = (_lib or lib()).solar_linear_attention_fwd(
-        B, T, H, d, dtype_code(dt), q.data_ptr(), ss[0], k.data_ptr(), ss[1], v.data_ptr(), ss[2], log_decay.data_ptr(), float(scale),
-        _ptr(lengths), _ptr(state0), O.data_ptr(), so, state.data_ptr(), _stream_on(dev, stream))
+        B, T, H, d, dtype_code(dt), q.data_ptr(), sq, k.data_ptr(), sk, v.data_ptr(), sv, log_decay.data_ptr(), float(scale),
+        _ptr(lengths), _ptr(state0), O.data_ptr(), so, state.data_ptr(), _stream(stream))
     if st:
         _check(st, "solar_linear_attention_fwd")
     return O, state
@@ -486,23 +495,23 @@ def linear_attention_fwd(q, k, v, log_decay, scale, state0=None, lengths=None, O
 def linear_attention_bwd(q, k, v, log_decay, scale, dO, state0=None, dstate=None, lengths=None, dq=None, dk=None, dv=None,
                          dstate0=None, stream=None):
     """solar_linear_attention_bwd -> dq, dk, dv [B,T,H,d] and dstate0 [B,H,d,d] fp32."""
-    B, T, H, d = q.shape
-    dt, dev, shape = q.dtype, q.device, q.shape
-    si = [_strides(t, n, shape, dt, dev) for t, n in ((q, "q"), (k, "k"), (v, "v"), (dO, "dO"))]
-    _need_on(log_decay, (H,), _F32, "log_decay", dev)
+    dt, dev, shape = q.dtype, _device_of(q, "q", 4), q.shape
+    B, T, H, d = shape
+    si = [_tokens(t, n, shape, dt, dev) for t, n in ((q, "q"), (k, "k"), (v, "v"), (dO, "dO"))]
+    _dense(log_decay, (H,), _F32, "log_decay", dev)
     if lengths is not None:
-        _need_on(lengths, (B,), _I32, "lengths", dev)
+        _dense(lengths, (B,), _I32, "lengths", dev)
     for t, n in ((state0, "state0"), (dstate, "dstate"), (dstate0, "dstate0")):
         if t is not None:
-            _need_on(t, (B, H, d, d), _F32, n, dev)
-    dq, dk, dv = (_tokens_like(q) if t is None else t for t in (dq, dk, dv))
-    so = [_strides(t, n, shape, dt, dev) for t, n in ((dq, "dq"), (dk, "dk"), (dv, "dv"))]
+            _dense(t, (B, H, d, d), _F32, n, dev)
+    dq, dk, dv = (q.new_empty(shape) if t is None else t for t in (dq, dk, dv))
+    so = [_tokens(t, n, shape, dt, dev) for t, n in ((dq, "dq"), (dk, "dk"), (dv, "dv"))]
     if dstate0 is None:
-        dstate0 = _empty((B, H, d, d), dtype=_F32, device=dev)
+        dstate0 = q.new_empty((B, H, d, d), dtype=_F32)
     st = (_lib or lib()).solar_linear_attention_bwd(
         B, T, H, d, dtype_code(dt), q.data_ptr(), si[0], k.data_ptr(), si[1], v.data_ptr(), si[2], log_decay.data_ptr(), float(scale),
         _ptr(lengths), _ptr(state0), dO.data_ptr(), si[3], _ptr(dstate), dq.data_ptr(), so[0], dk.data_ptr(), so[1],
-        dv.data_ptr(), so[2], dstate0.data_ptr(), _stream_on(dev, stream))
+        dv.data_ptr(), so[2], dstate0.data_ptr(), _stream(stream))
     if st:
         _check(st, "solar_linear_attention_bwd")
     return dq, dk, dv, dstate0
@@ -510,23 +519,26 @@ def linear_attention_bwd(q, k, v, log_decay, scale, dO, state0=None, dstate=None
 
 def linear_attention_step(q, k, v, log_decay, scale, state, O=None, stream=None):
     """solar_linear_attention_step: one event per user, q, k, v [B,H,d]; `state` [B,H,d,d] fp32 is updated in place."""
-    B, H, d = q.shape
-    dt, dev, shape = q.dtype, q.device, q.shape
-    ss = [_strides(t, n, shape, dt, dev) for t, n in ((q, "q"), (k, "k"), (v, "v"))]
-    _need_on(log_decay, (H,), _F32, "log_decay", dev)
-    _need_on(state, (B, H, d, d), _F32, "state", dev)
+    dt, dev, shape = q.dtype, _device_of(q, "q", 3), q.shape
+    B, H, d = shape
+    sq, sk, sv = _tokens(q, "q", shape, dt, dev), _tokens(k, "k", shape, dt, dev), _tokens(v, "v", shape, dt, dev)
+    _dense(log_decay, (H,), _F32, "log_decay", dev)
+    _dense(state, (B, H, d, d), _F32, "state", dev)
     if O is None:
-        O = _tokens_like(q)
-    so = _strides(O, "O", shape, dt, dev)
+        O = q.new_empty(shape)
+    so = _tokens(O, "O", shape, dt, dev)
     st = (_lib or lib()).solar_linear_attention_step(
-        B, H, d, dtype_code(dt), q.data_ptr(), ss[0], k.data_ptr(), ss[1], v.data_ptr(), ss[2], log_decay.data_ptr(), float(scale),
-        state.data_ptr(), O.data_ptr(), so, _stream_on(dev, stream))
+        B, H, d, dtype_code(dt), q.data_ptr(), sq, k.data_ptr(), sk, v.data_ptr(), sv, log_decay.data_ptr(), float(scale),
+        state.data_ptr(), O.data_ptr(), so, _stream(stream))
     if st:
         _check(st, "solar_linear_attention_step")
     return O
 
 
 # ---- a history in 8 bits ---------------------------------------------------------------------------
+_E4M3 = torch.float8_e4m3fn
+
+
 class HistoryCache(NamedTuple):
     """The cache of B users: k, v [B,H,N,d] float8_e4m3fn and the scales [B,H,N/64] fp32 of their blocks of 64 rows."""
     k: torch.Tensor
@@ -538,34 +550,38 @@ class HistoryCache(NamedTuple):
 def history_cache(B, H, N, d, device="cuda") -> HistoryCache:
     """An empty cache; N (rows per user and head) is rounded up to whole blocks."""
     N = -(-N // CACHE_BLOCK) * CACHE_BLOCK
-    rows = [_empty((B, H, N, d), dtype=torch.float8_e4m3fn, device=device) for _ in range(2)]
+    rows = [_empty((B, H, N, d), dtype=_E4M3, device=device) for _ in range(2)]
     return HistoryCache(*rows, *(torch.zeros((B, H, N // CACHE_BLOCK), dtype=_F32, device=device) for _ in range(2)))
 
 
-def _need_cache(cache, device):
+def _cache_sizes(cache, dev):
     k, v, ks, vs = cache
-    B, H, N, d = k.shape
+    shape = k.shape
+    if len(shape) != 4:
+        raise ValueError(f"cache.k: want four dimensions, got {tuple(shape)}")
+    B, H, N, d = shape
     blocks = (B, H, N // CACHE_BLOCK)
-    for t, n, shape, dtype in ((k, "k", k.shape, torch.float8_e4m3fn), (v, "v", k.shape, torch.float8_e4m3fn), (ks, "k_scale", blocks, _F32),
-                               (vs, "v_scale", blocks, _F32)):
-        _need_on(t, shape, dtype, "cache." + n, device)
+    _dense(k, shape, _E4M3, "cache.k", dev)
+    _dense(v, shape, _E4M3, "cache.v", dev)
+    _dense(ks, blocks, _F32, "cache.k_scale", dev)
+    _dense(vs, blocks, _F32, "cache.v_scale", dev)
     return B, H, N, d
 
 
 def history_cache_append(k, v, cache, start, counts=None, stream=None):
     """solar_history_cache_append: rows k, v [B,T,H,d] into `cache` from row start[b] on (the first counts[b] of them)."""
-    dt, dev, shape = k.dtype, k.device, k.shape
-    B, H, N, d = _need_cache(cache, dev)
+    dt, dev, shape = k.dtype, _device_of(k, "k", 4), k.shape
+    B, H, N, d = _cache_sizes(cache, dev)
     T = shape[1]
-    if tuple(shape) != (B, T, H, d):
+    if shape != (B, T, H, d):
         raise ValueError(f"k: want {(B, T, H, d)} for this cache, got {tuple(shape)}")
-    sk, sv = _strides(k, "k", shape, dt, dev), _strides(v, "v", shape, dt, dev)
-    _need_on(start, (B,), _I32, "start", dev)
+    sk, sv = _tokens(k, "k", shape, dt, dev), _tokens(v, "v", shape, dt, dev)
+    _dense(start, (B,), _I32, "start", dev)
     if counts is not None:
-        _need_on(counts, (B,), _I32, "counts", dev)
+        _dense(counts, (B,), _I32, "counts", dev)
     st = (_lib or lib()).solar_history_cache_append(
         B, T, H, N, d, dtype_code(dt), k.data_ptr(), sk, v.data_ptr(), sv, start.data_ptr(), _ptr(counts), cache[0].data_ptr(),
-        cache[1].data_ptr(), cache[2].data_ptr(), cache[3].data_ptr(), _stream_on(dev, stream))
+        cache[1].data_ptr(), cache[2].data_ptr(), cache[3].data_ptr(), _stream(stream))
     if st:
         _check(st, "solar_history_cache_append")
 
@@ -573,19 +589,19 @@ def history_cache_append(k, v, cache, start, counts=None, stream=None):
 def history_cache_attention(q, cache, lengths, scale, flags=0, O=None, stream=None):
     """solar_history_cache_attention: q [B,M,Hq,d] over the first lengths[b] rows of `cache` -> O [B,M,Hq,d].
     FLAG_CAUSAL: the queries are the last M rows."""
-    dt, dev, shape = q.dtype, q.device, q.shape
-    B, H, N, d = _need_cache(cache, dev)
+    dt, dev, shape = q.dtype, _device_of(q, "q", 4), q.shape
+    B, H, N, d = _cache_sizes(cache, dev)
     M, Hq = shape[1], shape[2]
-    if tuple(shape) != (B, M, Hq, d):
+    if shape != (B, M, Hq, d):
         raise ValueError(f"q: want {(B, M, Hq, d)} for this cache, got {tuple(shape)}")
-    sq = _strides(q, "q", shape, dt, dev)
-    _need_on(lengths, (B,), _I32, "lengths", dev)
+    sq = _tokens(q, "q", shape, dt, dev)
+    _dense(lengths, (B,), _I32, "lengths", dev)
     if O is None:
-        O = _tokens_like(q)
-    so = _strides(O, "O", shape, dt, dev)
+        O = q.new_empty(shape)
+    so = _tokens(O, "O", shape, dt, dev)
     st = (_lib or lib()).solar_history_cache_attention(
         B, M, Hq, H, N, d, dtype_code(dt), q.data_ptr(), sq, cache[0].data_ptr(), cache[1].data_ptr(), cache[2].data_ptr(),
-        cache[3].data_ptr(), lengths.data_ptr(), float(scale), int(flags), O.data_ptr(), so, _stream_on(dev, stream))
+        cache[3].data_ptr(), lengths.data_ptr(), float(scale), int(flags), O.data_ptr(), so, _stream(stream))
     if st:
         _check(st, "solar_history_cache_attention")
     return O

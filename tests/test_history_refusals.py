@@ -93,6 +93,9 @@ class Gpu:
         self.t = torch.zeros(*shape[:-1], 2 * shape[-1], dtype=dtype)[..., ::2] if strided else torch.zeros(shape, dtype=dtype)
         self.dtype, self.shape, self.is_cuda, self.device = dtype, self.t.shape, cuda, torch.device(device)
 
+    def get_device(self): return self.device.index if self.is_cuda else -1
+    def dim(self): return self.t.dim()
+    def new_empty(self, shape, dtype=None): return Gpu(*shape, dtype=dtype or self.dtype)
     def numel(self): return self.t.numel()
     def is_contiguous(self): return self.t.is_contiguous()
     def data_ptr(self): return self.t.data_ptr()
@@ -109,7 +112,8 @@ def calls(monkeypatch):
                 raise AttributeError(name)
             return lambda *a: (made.append((name, a)), 0)[1]
     monkeypatch.setattr(solar, "_lib", Recorder())
-    monkeypatch.setattr(solar, "_stream_on", lambda device, stream=None: 0)
+    monkeypatch.setattr(solar, "_stream", lambda stream=None: 0)
+    monkeypatch.setattr(solar, "_current_device", lambda: 0)
     return made
 
 
@@ -178,7 +182,19 @@ def test_strides_go_to_the_library(calls):
     assert args[6] is None and list(args[8]) == [T * 2 * H * d, 2 * H * d, d]
 
 
-def test_another_device_than_the_current_one_is_refused(monkeypatch):
-    monkeypatch.setattr(solar, "_current_device", lambda: 0)
+@pytest.mark.parametrize("call", ["fwd", "bwd", "step", "append", "attend"])
+def test_another_device_than_the_current_one_is_refused(calls, monkeypatch, call):
+    monkeypatch.setattr(solar, "_current_device", lambda: 1)
     with pytest.raises(ValueError, match="current device"):
-        solar._stream_on(torch.device("cuda:1"))
+        run(call, {n: Gpu(*s, dtype=t) for n, (s, t) in tensors(call).items()}, {n: Gpu(*s, dtype=t) for n, (s, t) in cache().items()})
+    assert not calls
+
+
+@pytest.mark.parametrize("call", ["fwd", "bwd", "step", "append", "attend"])
+def test_outputs_that_are_not_given_are_made(calls, call):
+    t = {n: Gpu(*s, dtype=x) for n, (s, x) in tensors(call).items()}
+    for n in ("O", "dq", "dk", "dv", "dstate0", "lengths", "counts", "state0", "dstate") + (() if call == "step" else ("state",)):
+        if n in t and (n != "lengths" or call != "attend"):
+            t[n] = None
+    run(call, t, {n: Gpu(*s, dtype=x) for n, (s, x) in cache().items()})
+    assert len(calls) == 1
