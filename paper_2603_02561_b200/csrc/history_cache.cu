@@ -13,9 +13,10 @@
 // group) rows per CTA, so that the query heads of a cached head share its rows.  Warps take blocks of 64 rows in
 // turn, each with its own running maximum and sum, and add up at the end; where the queries alone do not fill the
 // GPU, the rows are split over the CTAs of a cluster, which add up through distributed shared memory: one launch, no
-// workspace.  Rows go from global memory to registers as 8-bit fragments: a lane takes 16 bytes of a key, and the order
-// of the products' inner index is whatever those bytes are (queries are laid out to match); of the values it takes
-// the bytes of two rows that a fragment pairs, interleaved by one byte permutation.  All MMAs are fp16 x fp16 with fp32
+// workspace.  A warp brings its rows to shared memory itself, the keys of the next block and the values of this one while
+// it works on the keys of this one, and reads them as 8-bit fragments: a lane takes 16 bytes of a key, and the order of
+// the products' inner index is whatever those bytes are (queries are laid out to match); of the values it takes the bytes
+// of two rows that a fragment pairs, interleaved by one byte permutation.  All MMAs are fp16 x fp16 with fp32
 // sums, e4m3 being exact in fp16:
 //   q    each row by a power of two to below 2, then fp16 (bf16 storage: exact down to 2^-14 of the row's largest) or a
 //        high and a low fp16 half (fp32 storage: 22 bits)
@@ -142,15 +143,43 @@ template <int NP> __device__ __forceinline__ void split_half(float a, float b, u
   }
 }
 
-constexpr int kRowsPerCta = 16, kWarps = 4, kMaxSplits8 = 8;
+constexpr int kRowsPerCta = 16, kWarps = 4, kMaxSplits = 16;
 // CTAs that an SM is to hold, by registers
 template <typename T, int D> constexpr int kPerSm = D == 128 ? 2 : D == 64 || sizeof(T) == 4 ? 3 : 4;
 constexpr float kLift = 15.f;                      // log2 of the largest weight as fp16 holds it
 
 template <int D> struct HistShared {
-  float o[kWarps][kRowsPerCta][D];                 // the warps' sums; the first is the CTA's after they have joined
-  float m[kWarps][kRowsPerCta], l[kWarps][kRowsPerCta];
+  // A warp's rows on their way: keys of two blocks, values of one.
+  struct Ring { uint8_t k[2][kBlock * D], v[kBlock * D]; };
+  union {
+    Ring ring[kWarps];
+    struct {
+      float o[kWarps][kRowsPerCta][D];             // the warps' sums; the first is the CTA's after they have joined
+      float m[kWarps][kRowsPerCta], l[kWarps][kRowsPerCta];
+    };
+  };
 };
+// Which row of eight a column of the score fragment is (lane groups read keys by it, and values in its order), and
+// where a row's 16-byte pieces lie, so that no two lanes of a read meet in a bank.  d = 128: a row is all banks; the four
+// values' rows of a read, and the two keys' rows of eight lanes, each differ by the exclusive or.  d = 64: a row is half
+// of the banks, so that even and odd rows have to take turns as well.  d = 32: values meet in pairs.
+template <int D> __device__ __forceinline__ int row_of(int col) { return D == 64 ? col ^ ((col >> 1) & 1) : col; }
+template <int D> __device__ __forceinline__ uint32_t piece_at(int row, int piece) {
+  const int x = D == 128 ? (row & 6) ^ ((row & 1) << 2) : D == 64 ? (row >> 1) & 2 : 0;
+  return (uint32_t)row * D + (uint32_t)((piece ^ x) << 4);
+}
+// One block's rows of 8 bits to shared memory, zeros for those that do not exist
+template <int D> __device__ __forceinline__ void fetch_rows(uint8_t* dst, const uint8_t* src, int left, int lane) {
+  const uint32_t to = ptx::smem_u32(dst);
+#pragma unroll
+  for (int i = 0; i < kBlock * D / 16 / 32; ++i) {
+    const int at = lane + i * 32, row = at / (D / 16), piece = at % (D / 16);
+    const int n = row < left ? 16 : 0;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + piece_at<D>(row, piece)), "l"(src + (row < left ? at * 16 : 0)), "r"(n) : "memory");
+  }
+}
+__device__ __forceinline__ void rows_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void rows_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kWarps * 32, kPerSm<T, D>)
@@ -231,11 +260,29 @@ history_attention_kernel(LinearOperand q, T* O, long long ob, long long ot, long
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[x][i][e] = 0.f;
 
-  for (int blk = b0 + warp; blk < b1; blk += kWarps) {
-    const uint8_t* kp = kc + (size_t)blk * kBlock * D;
-    const uint8_t* vp = vc + (size_t)blk * kBlock * D;
-    const float ks = ld_dep(ksc + blk), vs = ld_dep(vsc + blk);
+  typename HistShared<D>::Ring& ring = sh.ring[warp];
+  float ks = 0.f, vs = 0.f;
+  auto fetch_k = [&](int blk, int slot) {
+    if (blk < b1) fetch_rows<D>(ring.k[slot], kc + (size_t)blk * kBlock * D, len - blk * kBlock, lane);
+    rows_commit();
+  };
+  auto fetch_v = [&](int blk) {
+    if (blk < b1) fetch_rows<D>(ring.v, vc + (size_t)blk * kBlock * D, len - blk * kBlock, lane);
+    rows_commit();
+  };
+  if (b0 + warp < b1) { ks = ld_dep(ksc + b0 + warp); vs = ld_dep(vsc + b0 + warp); }
+  fetch_k(b0 + warp, 0);
+  fetch_v(b0 + warp);
+  int slot = 0;
+  for (int blk = b0 + warp; blk < b1; blk += kWarps, slot ^= 1) {
+    fetch_k(blk + kWarps, slot ^ 1);
+    float ks_next = 0.f, vs_next = 0.f;
+    if (blk + kWarps < b1) { ks_next = ld_dep(ksc + blk + kWarps); vs_next = ld_dep(vsc + blk + kWarps); }
+    const uint8_t* kp = ring.k[slot];
+    const uint8_t* vp = ring.v;
     const int left = len - blk * kBlock;           // rows of the block that exist
+    rows_wait<2>();                                // this block's keys (its values and the next keys may be on their way)
+    __syncwarp();
     float s[8][4];
 #pragma unroll
     for (int n = 0; n < 8; ++n) {
@@ -245,10 +292,10 @@ history_attention_kernel(LinearOperand q, T* O, long long ob, long long ot, long
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
         if constexpr (D < 64) {
-          const uint2 u = *reinterpret_cast<const uint2*>(kp + (n * 8 + g) * D + j * 8);
+          const uint2 u = *reinterpret_cast<const uint2*>(kp + piece_at<D>(n * 8 + row_of<D>(g), j >> 1) + (j & 1) * 8);
           w[0] = u.x; w[1] = u.y;
         } else {
-          const uint4 u = *reinterpret_cast<const uint4*>(kp + (n * 8 + g) * D + c * 64 + j * 16);
+          const uint4 u = *reinterpret_cast<const uint4*>(kp + piece_at<D>(n * 8 + row_of<D>(g), c * 4 + j));
           w[4 * c] = u.x; w[4 * c + 1] = u.y; w[4 * c + 2] = u.z; w[4 * c + 3] = u.w;
         }
       }
@@ -268,7 +315,7 @@ history_attention_kernel(LinearOperand q, T* O, long long ob, long long ot, long
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         float x = s[n][e] * f[e >> 1];
-        if (!whole && blk * kBlock + n * 8 + 2 * j + (e & 1) >= limit[e >> 1]) x = -INFINITY;
+        if (!whole && blk * kBlock + n * 8 + row_of<D>(2 * j + (e & 1)) >= limit[e >> 1]) x = -INFINITY;
         s[n][e] = x;
         top[e >> 1] = fmaxf(top[e >> 1], x);
       }
@@ -298,21 +345,22 @@ history_attention_kernel(LinearOperand q, T* O, long long ob, long long ot, long
 #pragma unroll
       for (int t = 0; t < NP; ++t) { pa[t][n >> 1][2 * (n & 1)] = a[t]; pa[t][n >> 1][2 * (n & 1) + 1] = c[t]; }
     }
+    rows_wait<1>();                                // this block's values
+    __syncwarp();
     bool odd = false;                              // a value of the block that is not finite
 #pragma unroll
     for (int x = 0; x < HALVES; ++x) {
-      uint32_t w[4][4][HALF / 32];                 // rows 16 t + 2j, + 1, + 8, + 9; bytes g * HALF / 8 ..
+      uint32_t w[4][4][HALF / 32];                 // the rows of columns 2j and 2j + 1 of two tiles; bytes g * HALF / 8 ..
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int at = t * 16 + 2 * j + (r & 1) + (r >> 1) * 8;
-          const uint8_t* p = vp + at * D + x * 64 + g * (HALF / 8);
+          const int at = t * 16 + (r >> 1) * 8 + row_of<D>(2 * j + (r & 1));
           if constexpr (HALF == 64) {
-            const uint2 u = at < left ? *reinterpret_cast<const uint2*>(p) : make_uint2(0, 0);
+            const uint2 u = *reinterpret_cast<const uint2*>(vp + piece_at<D>(at, x * 4 + (g >> 1)) + (g & 1) * 8);
             w[t][r][0] = u.x; w[t][r][HALF / 32 - 1] = u.y;
           } else {
-            w[t][r][0] = at < left ? *reinterpret_cast<const uint32_t*>(p) : 0u;
+            w[t][r][0] = *reinterpret_cast<const uint32_t*>(vp + piece_at<D>(at, g >> 2) + (g & 3) * 4);
           }
         }
       if (!whole) {
@@ -355,10 +403,17 @@ history_attention_kernel(LinearOperand q, T* O, long long ob, long long ot, long
           for (int i = 0; i < NI; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              if (blk * kBlock + at < limit[e >> 1] && (vp[at * D + x * 64 + (2 * j + (e & 1)) * (HALF / 8) + i] & 0x7f) == 0x7f)
-                o[x][i][e] = __int_as_float(0x7fffffff);
+              if (blk * kBlock + at < limit[e >> 1]) {
+                const int d = x * 64 + (2 * j + (e & 1)) * (HALF / 8) + i;
+                if ((vp[piece_at<D>(at, d >> 4) + (d & 15)] & 0x7f) == 0x7f) o[x][i][e] = __int_as_float(0x7fffffff);
+              }
     }
+    __syncwarp();                                  // everybody has read the values
+    fetch_v(blk + kWarps);
+    ks = ks_next; vs = vs_next;
   }
+  rows_wait<0>();
+  __syncthreads();                                 // the sums come to lie over the rows
 
   // ---- the warps' sums -----------------------------------------------------------------------------------
 #pragma unroll
@@ -419,9 +474,9 @@ history_attention_kernel(LinearOperand q, T* O, long long ob, long long ot, long
     const int r = at / (D / 4), piece = at % (D / 4);
     float top = -INFINITY, l = 0.f;
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-    float ms[kMaxSplits8], ls[kMaxSplits8];
+    float ms[kMaxSplits], ls[kMaxSplits];
 #pragma unroll
-    for (int w = 0; w < kMaxSplits8; ++w) {
+    for (int w = 0; w < kMaxSplits; ++w) {
       ms[w] = -INFINITY; ls[w] = 0.f;
       if (w < sets) {
         if (splits > 1) {
@@ -434,7 +489,7 @@ history_attention_kernel(LinearOperand q, T* O, long long ob, long long ot, long
       top = fmaxf(top, ms[w]);
     }
 #pragma unroll
-    for (int w = 0; w < kMaxSplits8; ++w) {
+    for (int w = 0; w < kMaxSplits; ++w) {
       if (w >= sets) break;
       const float f = weight(ms[w], top);
       const float4 y = splits > 1 ? ptx::ld_cluster_f4(&sh.o[0][r][piece * 4], w) : *reinterpret_cast<const float4*>(&sh.o[w & (kWarps - 1)][r][piece * 4]);
@@ -470,9 +525,17 @@ cudaError_t launch_attention_td(const HistoryCall& c, cudaStream_t st) {
   const cudaError_t e = set_kernel_limits(reinterpret_cast<const void*>(&history_attention_kernel<T, D>), smem, limits_set);
   if (e != cudaSuccess) return e;
   const long long tiles = ((long long)c.M * c.G + kRowsPerCta - 1) / kRowsPerCta, ctas = tiles * c.H * c.B;
+  static bool wide[kMaxDevicesCached] = {};        // clusters of sixteen
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return cudaErrorInvalidDevice;
+  if (dev >= kMaxDevicesCached || !wide[dev]) {
+    const cudaError_t w = cudaFuncSetAttribute(reinterpret_cast<const void*>(&history_attention_kernel<T, D>), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (w != cudaSuccess) return w;
+    if (dev < kMaxDevicesCached) wide[dev] = true;
+  }
   // the rows are split while the CTAs still run at once and each warp has a block to itself
   int splits = 1;
-  while (splits < kMaxSplits8 && ctas * splits * 2 <= (long long)kNumSMs * kPerSm<T, D> && c.N / kBlock >= splits * 2 * kWarps) splits *= 2;
+  while (splits < kMaxSplits && ctas * splits * 2 <= (long long)kNumSMs * kPerSm<T, D> && c.N / kBlock >= splits * 2 * kWarps) splits *= 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(tiles * splits), c.H, c.B);
   cfg.blockDim = dim3(kWarps * 32);
