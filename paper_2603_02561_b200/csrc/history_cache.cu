@@ -50,6 +50,13 @@ __device__ __forceinline__ uint32_t e4m3x2_to_half2(uint32_t two) {
   return r;
 }
 
+__device__ __forceinline__ uint2 e4m3x4_to_half4(uint32_t w) {
+  uint2 r;
+  asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\tcvt.rn.f16x2.e4m3x2 %1, hi;\n\t}"
+      : "=r"(r.x), "=r"(r.y) : "r"(w));
+  return r;
+}
+
 // ---- append -------------------------------------------------------------------------------------------
 template <typename T, int D>
 __global__ void __launch_bounds__(D == 32 ? 128 : 256)
@@ -126,7 +133,7 @@ history_append_kernel(LinearOperand k, LinearOperand v, int T_new, int N, const 
 
 // ---- attention ----------------------------------------------------------------------------------------
 __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -285,26 +292,30 @@ history_attention_kernel(LinearOperand q, T* O, long long ob, long long ot, long
     __syncwarp();
     float s[8][4];
 #pragma unroll
-    for (int n = 0; n < 8; ++n) {
+    for (int n = 0; n < 8; ++n)
 #pragma unroll
       for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
-      uint32_t w[KC * KW];
 #pragma unroll
-      for (int c = 0; c < KC; ++c) {
+    for (int c = 0; c < KC; ++c) {
+      uint32_t w[8][KW];                           // 16 (8) bytes of eight keys: the tiles' products are independent
+#pragma unroll
+      for (int n = 0; n < 8; ++n) {
         if constexpr (D < 64) {
           const uint2 u = *reinterpret_cast<const uint2*>(kp + piece_at<D>(n * 8 + row_of<D>(g), j >> 1) + (j & 1) * 8);
-          w[0] = u.x; w[1] = u.y;
+          w[n][0] = u.x; w[n][1] = u.y;
         } else {
           const uint4 u = *reinterpret_cast<const uint4*>(kp + piece_at<D>(n * 8 + row_of<D>(g), c * 4 + j));
-          w[4 * c] = u.x; w[4 * c + 1] = u.y; w[4 * c + 2] = u.z; w[4 * c + 3] = u.w;
+          w[n][0] = u.x; w[n][1] = u.y; w[n][KW - 2] = u.z; w[n][KW - 1] = u.w;
         }
       }
 #pragma unroll
-      for (int kk = 0; kk < KS; ++kk) {
-        const uint32_t y0 = e4m3x2_to_half2(w[kk] & 0xffffu), y1 = e4m3x2_to_half2(w[kk] >> 16);
+      for (int kk = 0; kk < KW; ++kk)
 #pragma unroll
-        for (int t = 0; t < NP; ++t) mma_f16(s[n], qa[t][kk], y0, y1);
-      }
+        for (int n = 0; n < 8; ++n) {
+          const uint2 y = e4m3x4_to_half4(w[n][kk]);
+#pragma unroll
+          for (int t = 0; t < NP; ++t) mma_f16(s[n], qa[t][c * KW + kk], y.x, y.y);
+        }
     }
     // scores in log2 units, masked by position (whatever lies behind the history does not count, NaN neither)
     float top[2] = {-INFINITY, -INFINITY};
@@ -376,24 +387,25 @@ history_attention_kernel(LinearOperand q, T* O, long long ob, long long ot, long
               w[t][r][c] &= ~nan;
             }
       }
+      float c[NI][4];
 #pragma unroll
-      for (int i = 0; i < NI; i += 2) {
-        float c0[4] = {0.f, 0.f, 0.f, 0.f}, c1[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < NI; ++i)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
+        for (int e = 0; e < 4; ++e) c[i][e] = 0.f;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < NI; i += 2) {
           const uint32_t sel = (i & 2) ? 0x7362u : 0x5140u;
-          const uint32_t u = __byte_perm(w[t][0][i >> 2], w[t][1][i >> 2], sel), v = __byte_perm(w[t][2][i >> 2], w[t][3][i >> 2], sel);
-          const uint32_t y0 = e4m3x2_to_half2(u & 0xffffu), y1 = e4m3x2_to_half2(v & 0xffffu);
-          const uint32_t z0 = e4m3x2_to_half2(u >> 16), z1 = e4m3x2_to_half2(v >> 16);
+          const uint2 y = e4m3x4_to_half4(__byte_perm(w[t][0][i >> 2], w[t][1][i >> 2], sel));
+          const uint2 z = e4m3x4_to_half4(__byte_perm(w[t][2][i >> 2], w[t][3][i >> 2], sel));
 #pragma unroll
-          for (int n = 0; n < NP; ++n) { mma_f16(c0, pa[n][t], y0, y1); mma_f16(c1, pa[n][t], z0, z1); }
+          for (int n = 0; n < NP; ++n) { mma_f16(c[i], pa[n][t], y.x, z.x); mma_f16(c[i + 1], pa[n][t], y.y, z.y); }
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          o[x][i][e] = fmaf(o[x][i][e], corr[e >> 1], vs * c0[e]);
-          o[x][i + 1][e] = fmaf(o[x][i + 1][e], corr[e >> 1], vs * c1[e]);
-        }
-      }
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[x][i][e] = fmaf(o[x][i][e], corr[e >> 1], vs * c[i][e]);
     }
     if (__any_sync(~0u, odd)) {
       for (int at = 0; at < min(left, kBlock); ++at)
