@@ -150,6 +150,15 @@ template <int NP> __device__ __forceinline__ void split_half(float a, float b, u
   }
 }
 
+// (x, y) *= f, and (x, y) = (x, y) * f + (a, b), each in one instruction
+__device__ __forceinline__ void mul2(float& x, float& y, float f) {
+  asm("{\n\t.reg .b64 a, b;\n\tmov.b64 a, {%0, %1};\n\tmov.b64 b, {%2, %2};\n\tmul.rn.f32x2 a, a, b;\n\tmov.b64 {%0, %1}, a;\n\t}" : "+f"(x), "+f"(y) : "f"(f));
+}
+__device__ __forceinline__ void fma2(float& x, float& y, float f, float a, float b) {
+  asm("{\n\t.reg .b64 u, v, w;\n\tmov.b64 u, {%0, %1};\n\tmov.b64 v, {%2, %2};\n\tmov.b64 w, {%3, %4};\n\tfma.rn.f32x2 u, u, v, w;\n\tmov.b64 {%0, %1}, u;\n\t}"
+      : "+f"(x), "+f"(y) : "f"(f), "f"(a), "f"(b));
+}
+
 constexpr int kRowsPerCta = 16, kWarps = 4, kMaxSplits = 16;
 // CTAs that an SM is to hold, by registers
 template <typename T, int D> constexpr int kPerSm = D == 128 ? 2 : D == 64 || sizeof(T) == 4 ? 3 : 4;
@@ -175,14 +184,23 @@ template <int D> __device__ __forceinline__ uint32_t piece_at(int row, int piece
   const int x = D == 128 ? (row & 6) ^ ((row & 1) << 2) : D == 64 ? (row >> 1) & 2 : 0;
   return (uint32_t)row * D + (uint32_t)((piece ^ x) << 4);
 }
-// One block's rows of 8 bits to shared memory, zeros for those that do not exist
+// One block's rows of 8 bits to shared memory, zeros for those that do not exist.  A turn of the warp is 512 bytes; the
+// place of a lane's piece repeats with every turn (d = 128: with every second one, four rows further on).
 template <int D> __device__ __forceinline__ void fetch_rows(uint8_t* dst, const uint8_t* src, int left, int lane) {
-  const uint32_t to = ptx::smem_u32(dst);
+  const uint32_t to = ptx::smem_u32(dst) + piece_at<D>(lane / (D / 16), lane % (D / 16));
+  const uint32_t to1 = D == 128 ? ptx::smem_u32(dst) + (piece_at<D>(lane / (D / 16), lane % (D / 16)) ^ 64) : to;
+  src += lane * 16;
+  if (left >= kBlock) {
 #pragma unroll
-  for (int i = 0; i < kBlock * D / 16 / 32; ++i) {
-    const int at = lane + i * 32, row = at / (D / 16), piece = at % (D / 16);
-    const int n = row < left ? 16 : 0;
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + piece_at<D>(row, piece)), "l"(src + (row < left ? at * 16 : 0)), "r"(n) : "memory");
+    for (int i = 0; i < kBlock * D / 512; ++i)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((i & 1 ? to1 : to) + i * 512), "l"(src + i * 512) : "memory");
+  } else {
+#pragma unroll
+    for (int i = 0; i < kBlock * D / 512; ++i) {
+      const bool held = lane / (D / 16) + i * (512 / D) < left;
+      const int n = held ? 16 : 0;
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((i & 1 ? to1 : to) + i * 512), "l"(held ? src + i * 512 : src), "r"(n) : "memory");
+    }
   }
 }
 __device__ __forceinline__ void rows_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -322,14 +340,18 @@ history_attention_kernel(LinearOperand q, T* O, long long ob, long long ot, long
     const float f[2] = {qs[0] * ks, qs[1] * ks};
     const bool whole = __all_sync(~0u, (blk + 1) * kBlock <= min(limit[0], limit[1]));
 #pragma unroll
+    for (int n = 0; n < 8; ++n) { mul2(s[n][0], s[n][1], f[0]); mul2(s[n][2], s[n][3], f[1]); }
+    if (!whole) {
+#pragma unroll
+      for (int n = 0; n < 8; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (blk * kBlock + n * 8 + row_of<D>(2 * j + (e & 1)) >= limit[e >> 1]) s[n][e] = -INFINITY;
+    }
+#pragma unroll
     for (int n = 0; n < 8; ++n)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float x = s[n][e] * f[e >> 1];
-        if (!whole && blk * kBlock + n * 8 + row_of<D>(2 * j + (e & 1)) >= limit[e >> 1]) x = -INFINITY;
-        s[n][e] = x;
-        top[e >> 1] = fmaxf(top[e >> 1], x);
-      }
+      for (int e = 0; e < 4; e += 2) top[e >> 1] = fmaxf(fmaxf(top[e >> 1], s[n][e]), s[n][e + 1]);
     float corr[2], ref[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -405,7 +427,10 @@ history_attention_kernel(LinearOperand q, T* O, long long ob, long long ot, long
 #pragma unroll
       for (int i = 0; i < NI; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[x][i][e] = fmaf(o[x][i][e], corr[e >> 1], vs * c[i][e]);
+        for (int e = 0; e < 4; e += 2) {
+          mul2(c[i][e], c[i][e + 1], vs);
+          fma2(o[x][i][e], o[x][i][e + 1], corr[e >> 1], c[i][e], c[i][e + 1]);
+        }
     }
     if (__any_sync(~0u, odd)) {
       for (int at = 0; at < min(left, kBlock); ++at)
