@@ -24,6 +24,8 @@
 //   fp32 storage: every operand is split into three bf16 terms (24 bits), six products each: fp32's own rounding.
 #include <cuda_bf16.h>
 
+#include <type_traits>
+
 #include "sm100_ptx.cuh"
 #include "solar_internal.cuh"
 
@@ -75,7 +77,7 @@ template <typename T, int D> struct LaCfg {
   static constexpr int NP = sizeof(T) == 2 ? 1 : 3;            // bf16 terms of an element
   static constexpr int NA = sizeof(T) == 2 ? 2 : 3;            // of a decayed key
   static constexpr int C = (NP == 3 && D == 128) ? 32 : 64;    // tokens of a chunk (fp32, d = 128: by shared memory)
-  static constexpr int NW = D == 128 ? 8 : 4, NT = NW * 32;
+  static constexpr int NW = D == 128 ? 8 : 4, NTS = NW * 32, NT = 2 * NTS;      // warps of the state, and as many of the outputs
   static constexpr int RW = C / 16, CW = NW / RW, OC = D / CW; // warps over rows and over columns of the output tile
   static constexpr int MT = D / 16, NH = NW / MT, SC = D / NH; // warps over rows and over columns of the state
   static constexpr int PITCH = 2 * D + 16;                     // bytes of a row: 16-byte pieces, no bank conflicts
@@ -83,15 +85,17 @@ template <typename T, int D> struct LaCfg {
   static constexpr int STAGES = NP == 1 ? 2 : 1;
   static constexpr int SBUF = NP == 1 ? 2 : 1;                 // copies of the state as an operand
   static constexpr int STATE = NP * D * PITCH;
-  static constexpr int OFF_S = STAGES * 3 * OPER, OFF_W = OFF_S + SBUF * STATE;
+  static constexpr int SLOTS = NP == 1 ? 8 : 4;                // keys and values of two pairs of chunks, or of one
+  static constexpr int OFF_S = STAGES * 3 * OPER, OFF_W = SLOTS * OPER > OFF_S + SBUF * STATE ? SLOTS * OPER : OFF_S + SBUF * STATE;
   static constexpr int OFF_K = OFF_W + (C + 4) * 4;            // the keys' weights
   static constexpr size_t SMEM = OFF_K + 2 * C * sizeof(float);
-  static constexpr int PER_SM = SMEM <= 56 * 1024 ? 4 : SMEM <= 75 * 1024 ? 3 : SMEM <= 113 * 1024 ? 2 : 1;
+  static constexpr int PER_SM = D == 32 && NP == 1 ? 3 : D < 128 ? 2 : 1;
+  static_assert(PER_SM * (SMEM + 1024) <= 228 * 1024, "shared memory");
   static_assert(STAGES * 3 * OPER >= D * D * 4, "the segments' states lie over the tiles");
 };
 
 template <typename T, int D>
-__global__ void __launch_bounds__(LaCfg<T, D>::NT, LaCfg<T, D>::PER_SM > 3 ? 3 : LaCfg<T, D>::PER_SM)
+__global__ void __launch_bounds__(LaCfg<T, D>::NT, LaCfg<T, D>::PER_SM)
 linear_attention_kernel(const __grid_constant__ LinearParams prm) {
   using F = LaCfg<T, D>;
   constexpr int C = F::C, NP = F::NP, NA = F::NA, NT = F::NT, PITCH = F::PITCH;
@@ -99,7 +103,8 @@ linear_attention_kernel(const __grid_constant__ LinearParams prm) {
   const uint32_t sbase = ptx::smem_u32(smem);
   float* sw = reinterpret_cast<float*>(smem + F::OFF_W);       // g^0 .. g^C
   float* swk = reinterpret_cast<float*>(smem + F::OFF_K);      // what a chunk's keys enter the state with, then zeros
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, j = lane & 3;
+  const int tid = threadIdx.x, warp = (tid >> 5) % F::NW, lane = tid & 31, g = lane >> 2, j = lane & 3;
+  const bool state_warp = tid < F::NTS;
   const int seg = blockIdx.x, segs = gridDim.x;
   const int h = blockIdx.y / prm.roles, b = blockIdx.z;
   const LinearRole& R = prm.role[blockIdx.y % prm.roles];
@@ -155,6 +160,41 @@ linear_attention_kernel(const __grid_constant__ LinearParams prm) {
     }
   };
 
+  const uint32_t tile0 = sbase;
+  auto oper = [&](int stage, int which) { return tile0 + (uint32_t)(stage * 3 + which) * F::OPER; };
+  auto all = [&] { asm volatile("bar.sync 1, %0;" ::"n"(NT) : "memory"); };     // every warp of the CTA, wherever it stands
+  auto load_kv = [&](int c, int stage) { load(kp, R.k.st, c, oper(stage, 1)); load(vp, R.v.st, c, oper(stage, 2)); };
+  const int ldm_r = lane & 7, ldm_m = lane >> 3;
+  const uint32_t off_mn = (uint32_t)((((ldm_m >> 1) * 8 + ldm_r) * PITCH) + (ldm_m & 1) * 16);   // rows by bit 1, columns by bit 0
+  const uint32_t off_nm = (uint32_t)((((ldm_m & 1) * 8 + ldm_r) * PITCH) + (ldm_m >> 1) * 16);   // rows by bit 0, columns by bit 1
+  // The chunks of a loop: `before` a chunk's tiles are needed, and `after` they have been read (bf16: the next chunk is on
+  // its way meanwhile).  Both kinds of warps walk through them with the same barriers.
+  auto start = [&](int c) {
+    if (NP != 1 || c >= c1) return;
+    load(qp, R.q.st, c, oper(0, 0));
+    load_kv(c, 0);
+    cp_async_commit();
+  };
+  auto before = [&](int c) {
+    const int stage = NP == 1 ? (c - c0) & 1 : 0;
+    if constexpr (NP == 1) {
+      cp_async_wait<0>();
+      all();
+      if (c + 1 < c1) {
+        load(qp, R.q.st, c + 1, oper(stage ^ 1, 0));
+        load_kv(c + 1, stage ^ 1);
+        cp_async_commit();
+      }
+    } else {
+      load(qp, R.q.st, c, oper(0, 0));
+      load_kv(c, 0);
+      all();
+    }
+    return stage;
+  };
+  auto after = [&] { if constexpr (NP != 1) all(); };
+  all();                                                           // the powers
+
   // ---- the state: this warp's 16 rows x SC columns ---------------------------------------------------
   const int mt = warp % F::MT, nh = warp / F::MT;
   float st[F::SC / 8][4];
@@ -162,10 +202,6 @@ linear_attention_kernel(const __grid_constant__ LinearParams prm) {
   for (int n = 0; n < F::SC / 8; ++n)
 #pragma unroll
     for (int i = 0; i < 4; ++i) st[n][i] = 0.f;
-  const int ldm_r = lane & 7, ldm_m = lane >> 3;
-  const uint32_t off_mn = (uint32_t)((((ldm_m >> 1) * 8 + ldm_r) * PITCH) + (ldm_m & 1) * 16);   // rows by bit 1, columns by bit 0
-  const uint32_t off_nm = (uint32_t)((((ldm_m & 1) * 8 + ldm_r) * PITCH) + (ldm_m >> 1) * 16);   // rows by bit 0, columns by bit 1
-
   auto update = [&](uint32_t sk, uint32_t sv, int n_real) {
     const float gn = sw[n_real];
 #pragma unroll
@@ -207,233 +243,294 @@ linear_attention_kernel(const __grid_constant__ LinearParams prm) {
     }
   };
 
-  const uint32_t tile0 = sbase;
-  auto oper = [&](int stage, int which) { return tile0 + (uint32_t)(stage * 3 + which) * F::OPER; };
-
-  // ---- the state before this segment ----------------------------------------------------------------
-  const size_t state_at = ((size_t)b * prm.H + h) * D * D;
-  auto state_row = [&](int i) { return mt * 16 + g + (i >> 1) * 8; };
-  auto state_col = [&](int n, int i) { return nh * F::SC + n * 8 + 2 * j + (i & 1); };
-  if (segs > 1) {
-    __syncthreads();
-    if (seg < segs - 1) {
-      if (NP == 1 && c0 < c1) { load(kp, R.k.st, c0, oper(0, 1)); load(vp, R.v.st, c0, oper(0, 2)); cp_async_commit(); }
-      for (int c = c0; c < c1; ++c) {
-        const int stage = NP == 1 ? (c - c0) & 1 : 0;
-        if constexpr (NP == 1) {
-          cp_async_wait<0>();
-          __syncthreads();
-          if (c + 1 < c1) { load(kp, R.k.st, c + 1, oper(stage ^ 1, 1)); load(vp, R.v.st, c + 1, oper(stage ^ 1, 2)); cp_async_commit(); }
-        } else {
-          __syncthreads();
-          load(kp, R.k.st, c, oper(0, 1)); load(vp, R.v.st, c, oper(0, 2));
-          __syncthreads();
-        }
-        update(oper(stage, 1), oper(stage, 2), min(C, len - c * C));
+  // ---- the segment's own state, where somebody needs it: both kinds of warps, a chunk of a pair each ------------
+  if (segs > 1 && seg < segs - 1) {
+    const int pairs = (c1 - c0 + 1) / 2;
+    auto slot = [&](int pair, int half, int which) { return tile0 + (uint32_t)((NP == 1 ? (pair & 1) * 4 : 0) + half * 2 + which) * F::OPER; };
+    auto load_pair = [&](int pair) {
+      for (int half = 0; half < 2 && c0 + 2 * pair + half < c1; ++half) {
+        load(kp, R.k.st, c0 + 2 * pair + half, slot(pair, half, 0));
+        load(vp, R.v.st, c0 + 2 * pair + half, slot(pair, half, 1));
       }
-      __syncthreads();
-      float4* mine = reinterpret_cast<float4*>(smem);
+      if (NP == 1) cp_async_commit();
+    };
+    auto fade = [&](float f) {
 #pragma unroll
-      for (int n = 0; n < F::SC / 8; ++n) mine[n * NT + tid] = make_float4(st[n][0], st[n][1], st[n][2], st[n][3]);
+      for (int n = 0; n < F::SC / 8; ++n) { mul2(st[n][0], st[n][1], f); mul2(st[n][2], st[n][3], f); }
+    };
+    if (NP == 1) load_pair(0);
+    for (int pair = 0; pair < pairs; ++pair) {
+      if constexpr (NP == 1) {
+        cp_async_wait<0>();
+        all();
+        if (pair + 1 < pairs) load_pair(pair + 1);
+      } else {
+        load_pair(pair);
+        all();
+      }
+      const int at = (c0 + 2 * pair) * C, n0 = min(C, len - at), n1 = c0 + 2 * pair + 1 < c1 ? min(C, len - at - C) : 0;
+      if (!state_warp) fade(sw[n0]);
+      const int mine = state_warp ? n0 : n1;
+      if (mine > 0) update(slot(pair, state_warp ? 0 : 1, 0), slot(pair, state_warp ? 0 : 1, 1), mine);
+      if (state_warp) fade(sw[n1]);
+      if (NP != 1) all();
     }
-    ptx::cluster_sync();
+    // one sum of the two: this CTA's, for the cluster
+    all();
+    float4* own = reinterpret_cast<float4*>(smem) + tid % F::NTS;
+    if (!state_warp) {
 #pragma unroll
-    for (int n = 0; n < F::SC / 8; ++n)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) st[n][i] = 0.f;
-    const int before = min(c0 * C, len);
-    for (int m = 0; m < seg; ++m) {                                // in the segments' order
-      const int end = min(min((m + 1) * per, chunks) * C, len);
-      const float f = power(before - end);
-      if (m * per >= chunks) break;
+      for (int n = 0; n < F::SC / 8; ++n) own[n * F::NTS] = make_float4(st[n][0], st[n][1], st[n][2], st[n][3]);
+    }
+    all();
+    if (state_warp) {
 #pragma unroll
       for (int n = 0; n < F::SC / 8; ++n) {
-        const float4 e = ptx::ld_cluster_f4(reinterpret_cast<const float4*>(smem) + n * NT + tid, m);
-        st[n][0] = fmaf(f, e.x, st[n][0]); st[n][1] = fmaf(f, e.y, st[n][1]);
-        st[n][2] = fmaf(f, e.z, st[n][2]); st[n][3] = fmaf(f, e.w, st[n][3]);
+        const float4 e = own[n * F::NTS];
+        own[n * F::NTS] = make_float4(st[n][0] + e.x, st[n][1] + e.y, st[n][2] + e.z, st[n][3] + e.w);
       }
     }
-    ptx::cluster_sync();                                           // the tiles may be written again
-  }
-  if (R.s0 != nullptr) {
-    const float f = power(min(c0 * C, len));
-#pragma unroll
-    for (int n = 0; n < F::SC / 8; ++n)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        st[n][i] = fmaf(f, ld_dep(R.s0 + state_at + (size_t)state_row(i) * R.s0_r + (size_t)state_col(n, i) * R.s0_c), st[n][i]);
   }
 
-  // The state as an operand: its accumulators rounded to NP bf16 terms
-  auto put_state = [&](int buf) {
+  if (state_warp) {
+    // ---- the state before this segment ----------------------------------------------------------------
+    const size_t state_at = ((size_t)b * prm.H + h) * D * D;
+    auto state_row = [&](int i) { return mt * 16 + g + (i >> 1) * 8; };
+    auto state_col = [&](int n, int i) { return nh * F::SC + n * 8 + 2 * j + (i & 1); };
+    if (segs > 1) {
+      ptx::cluster_sync();
 #pragma unroll
-    for (int n = 0; n < F::SC / 8; ++n)
+      for (int n = 0; n < F::SC / 8; ++n)
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        uint32_t y[NP];
-        split<NP>(st[n][2 * half], st[n][2 * half + 1], y);
+        for (int i = 0; i < 4; ++i) st[n][i] = 0.f;
+      const int rows = min(c0 * C, len);
+      for (int m = 0; m < seg; ++m) {                              // in the segments' order
+        const int end = min(min((m + 1) * per, chunks) * C, len);
+        const float f = power(rows - end);
+        if (m * per >= chunks) break;
 #pragma unroll
-        for (int p = 0; p < NP; ++p)
-          *reinterpret_cast<uint32_t*>(smem + F::OFF_S + buf * F::STATE + p * D * PITCH + state_row(2 * half) * PITCH + state_col(n, 0) * 2) = y[p];
-      }
-  };
-
-  // ---- outputs, chunk by chunk ------------------------------------------------------------------------
-  // (rows further down have more keys: the two column halves' warps of a scheduler, or the CTAs of an SM, take turns)
-  const int cw = warp / F::RW, rw0 = warp % F::RW, rw = F::CW > 1 ? (cw & 1 ? F::RW - 1 - rw0 : rw0) : (warp + seg + h) % F::RW;
-  // What this thread's eight scores of a 16 x 16 tile are multiplied by: on the diagonal (zero above it), and, but for a
-  // power of g^16, below it.
-  float near[8], far[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int gap = g + ((i >> 1) & 1) * 8 - (2 * j + (i & 1) + (i >> 2) * 8);
-    near[i] = gap >= 0 ? R.ap * power(gap) : 0.f;
-    far[i] = R.ap * power(16 + gap);
-  }
-  if (c0 < c1) {
-    put_state(0);
-    if (NP == 1) {
-      load(qp, R.q.st, c0, oper(0, 0)); load(kp, R.k.st, c0, oper(0, 1)); load(vp, R.v.st, c0, oper(0, 2));
-      cp_async_commit();
-    }
-  }
-  for (int c = c0; c < c1; ++c) {
-    const int stage = NP == 1 ? (c - c0) & 1 : 0, buf = F::SBUF == 2 ? (c - c0) & 1 : 0;
-    if constexpr (NP == 1) {
-      cp_async_wait<0>();
-      __syncthreads();
-      if (c + 1 < c1) {
-        load(qp, R.q.st, c + 1, oper(stage ^ 1, 0)); load(kp, R.k.st, c + 1, oper(stage ^ 1, 1)); load(vp, R.v.st, c + 1, oper(stage ^ 1, 2));
-        cp_async_commit();
-      }
-    } else {
-      load(qp, R.q.st, c, oper(0, 0)); load(kp, R.k.st, c, oper(0, 1)); load(vp, R.v.st, c, oper(0, 2));
-      __syncthreads();
-    }
-    const uint32_t sq = oper(stage, 0), sk = oper(stage, 1), sv = oper(stage, 2), ss = sbase + F::OFF_S + buf * F::STATE;
-    const int n_real = min(C, len - c * C);
-
-    float o[F::OC / 8][4];
-#pragma unroll
-    for (int n = 0; n < F::OC / 8; ++n)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) o[n][i] = 0.f;
-    uint32_t q[NP][D / 16][4];
-#pragma unroll
-    for (int p = 0; p < NP; ++p)
-#pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) ldsm(q[p][ks], sq + p * F::TILE + rw * 16 * PITCH + ks * 32 + off_nm);
-    // q S, then its rows' powers
-#pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks)
-#pragma unroll
-      for (int n2 = 0; n2 < F::OC / 16; ++n2)
-#pragma unroll
-        for (int pb = 0; pb < NP; ++pb) {
-          uint32_t y[4];
-          ldsm_t(y, ss + pb * D * PITCH + ks * 16 * PITCH + (cw * F::OC + n2 * 16) * 2 + off_nm);
-#pragma unroll
-          for (int pa = 0; pa < NP; ++pa)
-            if (pa + pb < NP) {
-              mma(o[2 * n2], q[pa][ks], y[0], y[1]);
-              mma(o[2 * n2 + 1], q[pa][ks], y[2], y[3]);
-            }
+        for (int n = 0; n < F::SC / 8; ++n) {
+          const float4 e = ptx::ld_cluster_f4(reinterpret_cast<const float4*>(smem) + n * F::NTS + tid, m);
+          st[n][0] = fmaf(f, e.x, st[n][0]); st[n][1] = fmaf(f, e.y, st[n][1]);
+          st[n][2] = fmaf(f, e.z, st[n][2]); st[n][3] = fmaf(f, e.w, st[n][3]);
         }
-    const int t0 = rw * 16 + g, t1 = t0 + 8;
-    {
-      const float f0 = R.aq * sw[t0 + 1 - rev], f1 = R.aq * sw[t1 + 1 - rev];
-#pragma unroll
-      for (int n = 0; n < F::OC / 8; ++n) { mul2(o[n][0], o[n][1], f0); mul2(o[n][2], o[n][3], f1); }
+      }
+      ptx::cluster_sync();                                         // the tiles may be written again
     }
-    // scores of 16 keys at a time, decayed, times their values
+    if (R.s0 != nullptr) {
+      const float f = power(min(c0 * C, len));
 #pragma unroll
-    for (int kt = 0; kt < C / 16; ++kt) {
-      if (kt > rw) break;
-      float p0[4], p1[4];
-      {
-        float z[2][2][4];                          // two chains for each half of the keys
+      for (int n = 0; n < F::SC / 8; ++n)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) z[0][0][i] = z[0][1][i] = z[1][0][i] = z[1][1][i] = 0.f;
+        for (int i = 0; i < 4; ++i)
+          st[n][i] = fmaf(f, ld_dep(R.s0 + state_at + (size_t)state_row(i) * R.s0_r + (size_t)state_col(n, i) * R.s0_c), st[n][i]);
+    }
+    // The state as an operand: its accumulators rounded to NP bf16 terms
+    auto put_state = [&](int buf) {
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks)
+      for (int n = 0; n < F::SC / 8; ++n)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          uint32_t y[NP];
+          split<NP>(st[n][2 * half], st[n][2 * half + 1], y);
+#pragma unroll
+          for (int p = 0; p < NP; ++p)
+            *reinterpret_cast<uint32_t*>(smem + F::OFF_S + buf * F::STATE + p * D * PITCH + state_row(2 * half) * PITCH + state_col(n, 0) * 2) = y[p];
+        }
+    };
+    put_state(0);
+    start(c0);
+    for (int c = c0; c < c1; ++c) {
+      const int stage = before(c);
+      update(oper(stage, 1), oper(stage, 2), min(C, len - c * C));
+      after();
+      if (c + 1 < c1) put_state(F::SBUF == 2 ? (c + 1 - c0) & 1 : 0);
+    }
+    if (R.s1 != nullptr && seg == segs - 1) {
+#pragma unroll
+      for (int n = 0; n < F::SC / 8; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) R.s1[state_at + (size_t)state_row(i) * D + state_col(n, i)] = st[n][i];
+    }
+  } else {
+    // ---- outputs, chunk by chunk ----------------------------------------------------------------------
+    if (segs > 1) {
+      ptx::cluster_sync();
+      ptx::cluster_sync();
+    }
+    const int cw = warp / F::RW, rw0 = warp % F::RW, rw = F::CW > 1 ? (cw & 1 ? F::RW - 1 - rw0 : rw0) : (warp + seg + h) % F::RW;
+    // What this thread's eight scores of a 16 x 16 tile are multiplied by: on the diagonal (zero above it), and, but for a
+    // power of g^16, below it.
+    float near[8], far[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int gap = g + ((i >> 1) & 1) * 8 - (2 * j + (i & 1) + (i >> 2) * 8);
+      near[i] = gap >= 0 ? R.ap * power(gap) : 0.f;
+      far[i] = R.ap * power(16 + gap);
+    }
+    start(c0);
+    for (int c = c0; c < c1; ++c) {
+      const int stage = before(c), buf = F::SBUF == 2 ? (c - c0) & 1 : 0;
+      const uint32_t sq = oper(stage, 0), sk = oper(stage, 1), sv = oper(stage, 2), ss = sbase + F::OFF_S + buf * F::STATE;
+
+      float o[F::OC / 8][4];
+#pragma unroll
+      for (int n = 0; n < F::OC / 8; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[n][i] = 0.f;
+      uint32_t q[NP][D / 16][4];
+#pragma unroll
+      for (int p = 0; p < NP; ++p)
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) ldsm(q[p][ks], sq + p * F::TILE + rw * 16 * PITCH + ks * 32 + off_nm);
+      // q S, then its rows' powers
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+        for (int n2 = 0; n2 < F::OC / 16; ++n2)
 #pragma unroll
           for (int pb = 0; pb < NP; ++pb) {
             uint32_t y[4];
-            ldsm(y, sk + pb * F::TILE + kt * 16 * PITCH + ks * 32 + off_mn);
+            ldsm_t(y, ss + pb * D * PITCH + ks * 16 * PITCH + (cw * F::OC + n2 * 16) * 2 + off_nm);
 #pragma unroll
-            for (int pa = 0; pa < NP - pb; ++pa) {
-              mma(z[(ks + pa) & 1][0], q[pa][ks], y[0], y[1]);
-              mma(z[(ks + pa) & 1][1], q[pa][ks], y[2], y[3]);
+            for (int pa = 0; pa < NP; ++pa)
+              if (pa + pb < NP) {
+                mma(o[2 * n2], q[pa][ks], y[0], y[1]);
+                mma(o[2 * n2 + 1], q[pa][ks], y[2], y[3]);
+              }
+          }
+      const int t0 = rw * 16 + g, t1 = t0 + 8;
+      {
+        const float f0 = R.aq * sw[t0 + 1 - rev], f1 = R.aq * sw[t1 + 1 - rev];
+#pragma unroll
+        for (int n = 0; n < F::OC / 8; ++n) { mul2(o[n][0], o[n][1], f0); mul2(o[n][2], o[n][3], f1); }
+      }
+      // Scores of 16 keys at a time, decayed, times their values.  bf16: straight-line code for each number of tiles that
+      // a warp's rows have, so that the products of all of them are in flight together.
+      if constexpr (NP == 1) {
+        auto tiles = [&](auto number) {
+          constexpr int KT = decltype(number)::value;
+          float z[KT][2][4];
+#pragma unroll
+          for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[kt][0][i] = z[kt][1][i] = 0.f;
+#pragma unroll
+          for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) {
+              uint32_t y[4];
+              ldsm(y, sk + kt * 16 * PITCH + ks * 32 + off_mn);
+              mma(z[kt][0], q[0][ks], y[0], y[1]);
+              mma(z[kt][1], q[0][ks], y[2], y[3]);
+            }
+#pragma unroll
+          for (int kt = 0; kt < KT; ++kt) {
+            uint32_t a[4];
+            if (kt == KT - 1) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) { z[kt][0][i] *= near[i]; z[kt][1][i] *= near[4 + i]; }
+            } else {
+              const float f = sw[16 * (KT - 2 - kt)];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) { z[kt][0][i] *= f * far[i]; z[kt][1][i] *= f * far[4 + i]; }
+            }
+            a[0] = ptx::pack_bf16(z[kt][0][0], z[kt][0][1]); a[1] = ptx::pack_bf16(z[kt][0][2], z[kt][0][3]);
+            a[2] = ptx::pack_bf16(z[kt][1][0], z[kt][1][1]); a[3] = ptx::pack_bf16(z[kt][1][2], z[kt][1][3]);
+#pragma unroll
+            for (int n2 = 0; n2 < F::OC / 16; ++n2) {
+              uint32_t y[4];
+              ldsm_t(y, sv + kt * 16 * PITCH + (cw * F::OC + n2 * 16) * 2 + off_nm);
+              mma(o[2 * n2], a, y[0], y[1]);
+              mma(o[2 * n2 + 1], a, y[2], y[3]);
             }
           }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { p0[i] = z[0][0][i] + z[1][0][i]; p1[i] = z[0][1][i] + z[1][1][i]; }
-      }
-      if (kt == rw) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { p0[i] *= near[i]; p1[i] *= near[4 + i]; }
+        };
+        static_assert(F::RW == 4, "rows of a chunk over four warps");
+        if (rw == 0) tiles(std::integral_constant<int, 1>{});
+        else if (rw == 1) tiles(std::integral_constant<int, 2>{});
+        else if (rw == 2) tiles(std::integral_constant<int, 3>{});
+        else tiles(std::integral_constant<int, 4>{});
       } else {
-        const float f = sw[16 * (rw - kt - 1)];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { p0[i] *= f * far[i]; p1[i] *= f * far[4 + i]; }
-      }
-      uint32_t a[NP][4];
-      {
-        uint32_t y[NP];
-        split<NP>(p0[0], p0[1], y);
+      for (int kt = 0; kt < C / 16; ++kt) {
+        if (kt > rw) break;
+        float p0[4], p1[4];
+        {
+          float z[2][2][4];                          // two chains for each half of the keys
 #pragma unroll
-        for (int p = 0; p < NP; ++p) a[p][0] = y[p];
-        split<NP>(p0[2], p0[3], y);
+          for (int i = 0; i < 4; ++i) z[0][0][i] = z[0][1][i] = z[1][0][i] = z[1][1][i] = 0.f;
 #pragma unroll
-        for (int p = 0; p < NP; ++p) a[p][1] = y[p];
-        split<NP>(p1[0], p1[1], y);
+          for (int ks = 0; ks < D / 16; ++ks)
 #pragma unroll
-        for (int p = 0; p < NP; ++p) a[p][2] = y[p];
-        split<NP>(p1[2], p1[3], y);
+            for (int pb = 0; pb < NP; ++pb) {
+              uint32_t y[4];
+              ldsm(y, sk + pb * F::TILE + kt * 16 * PITCH + ks * 32 + off_mn);
 #pragma unroll
-        for (int p = 0; p < NP; ++p) a[p][3] = y[p];
-      }
-#pragma unroll
-      for (int n2 = 0; n2 < F::OC / 16; ++n2)
-#pragma unroll
-        for (int pb = 0; pb < NP; ++pb) {
-          uint32_t y[4];
-          ldsm_t(y, sv + pb * F::TILE + kt * 16 * PITCH + (cw * F::OC + n2 * 16) * 2 + off_nm);
-#pragma unroll
-          for (int pa = 0; pa < NP; ++pa)
-            if (pa + pb < NP) {
-              mma(o[2 * n2], a[pa], y[0], y[1]);
-              mma(o[2 * n2 + 1], a[pa], y[2], y[3]);
+              for (int pa = 0; pa < NP - pb; ++pa) {
+                mma(z[(ks + pa) & 1][0], q[pa][ks], y[0], y[1]);
+                mma(z[(ks + pa) & 1][1], q[pa][ks], y[2], y[3]);
+              }
             }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) { p0[i] = z[0][0][i] + z[1][0][i]; p1[i] = z[0][1][i] + z[1][1][i]; }
         }
-    }
+        if (kt == rw) {
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int at = c * C + (half ? t1 : t0);
-      if (at < len) {
-        T* row = op + (long long)(rev ? len - 1 - at : at) * R.ot + cw * F::OC + 2 * j;
+          for (int i = 0; i < 4; ++i) { p0[i] *= near[i]; p1[i] *= near[4 + i]; }
+        } else {
+          const float f = sw[16 * (rw - kt - 1)];
 #pragma unroll
-        for (int n = 0; n < F::OC / 8; ++n) {
-          if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t*>(row + n * 8) = ptx::pack_bf16(o[n][2 * half], o[n][2 * half + 1]);
-          else *reinterpret_cast<float2*>(row + n * 8) = make_float2(o[n][2 * half], o[n][2 * half + 1]);
+          for (int i = 0; i < 4; ++i) { p0[i] *= f * far[i]; p1[i] *= f * far[4 + i]; }
+        }
+        uint32_t a[NP][4];
+        {
+          uint32_t y[NP];
+          split<NP>(p0[0], p0[1], y);
+#pragma unroll
+          for (int p = 0; p < NP; ++p) a[p][0] = y[p];
+          split<NP>(p0[2], p0[3], y);
+#pragma unroll
+          for (int p = 0; p < NP; ++p) a[p][1] = y[p];
+          split<NP>(p1[0], p1[1], y);
+#pragma unroll
+          for (int p = 0; p < NP; ++p) a[p][2] = y[p];
+          split<NP>(p1[2], p1[3], y);
+#pragma unroll
+          for (int p = 0; p < NP; ++p) a[p][3] = y[p];
+        }
+#pragma unroll
+        for (int n2 = 0; n2 < F::OC / 16; ++n2)
+#pragma unroll
+          for (int pb = 0; pb < NP; ++pb) {
+            uint32_t y[4];
+            ldsm_t(y, sv + pb * F::TILE + kt * 16 * PITCH + (cw * F::OC + n2 * 16) * 2 + off_nm);
+#pragma unroll
+            for (int pa = 0; pa < NP; ++pa)
+              if (pa + pb < NP) {
+                mma(o[2 * n2], a[pa], y[0], y[1]);
+                mma(o[2 * n2 + 1], a[pa], y[2], y[3]);
+              }
+          }
+      }
+      }
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int at = c * C + (half ? t1 : t0);
+        if (at < len) {
+          T* row = op + (long long)(rev ? len - 1 - at : at) * R.ot + cw * F::OC + 2 * j;
+#pragma unroll
+          for (int n = 0; n < F::OC / 8; ++n) {
+            if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t*>(row + n * 8) = ptx::pack_bf16(o[n][2 * half], o[n][2 * half + 1]);
+            else *reinterpret_cast<float2*>(row + n * 8) = make_float2(o[n][2 * half], o[n][2 * half + 1]);
+          }
         }
       }
+      after();
     }
-    update(sk, sv, n_real);
-    if (c + 1 < c1) {
-      if constexpr (F::SBUF == 1) __syncthreads();                 // everybody has read the state before
-      put_state(F::SBUF == 2 ? buf ^ 1 : 0);
-    }
-    if constexpr (NP != 1) __syncthreads();                        // the tiles may be written again
   }
 
-  // ---- the last state, and the rows behind the sequence -----------------------------------------------
-  if (R.s1 != nullptr && seg == segs - 1) {
-#pragma unroll
-    for (int n = 0; n < F::SC / 8; ++n)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) R.s1[state_at + (size_t)state_row(i) * D + state_col(n, i)] = st[n][i];
-  }
+  // ---- the rows behind the sequence -------------------------------------------------------------------
   constexpr int PIECES = D * (int)sizeof(T) / 16;
   for (long long i = (long long)seg * NT + tid; i < (long long)(prm.T - len) * PIECES; i += (long long)segs * NT)
     *reinterpret_cast<uint4*>(op + (len + i / PIECES) * R.ot + (i % PIECES) * (16 / sizeof(T))) = make_uint4(0, 0, 0, 0);
