@@ -18,7 +18,7 @@
 // its outputs.  So there is no workspace, no second launch and no order that changes between runs.
 //
 // Arithmetic: warp-level bf16 MMAs, fp32 accumulators; the state lives in fp32 accumulators over the whole segment.
-//   bf16 storage: q, k, v enter as they are; g^(n-1-s) k is split into a high and a low bf16 half (16 bits: the state is
+//   bf16 storage: q, k, v enter as they are; g^(n-1-s) k is split into two or three bf16 terms (16 or 24 bits: the state is
 //   returned in fp32); the scores behind their decay and the state as an operand of q S are rounded to bf16, as the
 //   output will be.
 //   fp32 storage: every operand is split into three bf16 terms (24 bits), six products each: fp32's own rounding.
@@ -73,9 +73,37 @@ __device__ __forceinline__ void mul2(float& x, float& y, float f) {
   asm("{\n\t.reg .b64 a, b;\n\tmov.b64 a, {%0, %1};\n\tmov.b64 b, {%2, %2};\n\tmul.rn.f32x2 a, a, b;\n\tmov.b64 {%0, %1}, a;\n\t}" : "+f"(x), "+f"(y) : "f"(f));
 }
 
+// (x, y) = (x, y) f + (a, b)
+__device__ __forceinline__ void fma2(float& x, float& y, float f, float a, float b) {
+  asm("{\n\t.reg .b64 u, v, w;\n\tmov.b64 u, {%0, %1};\n\tmov.b64 v, {%2, %2};\n\tmov.b64 w, {%3, %4};\n\tfma.rn.f32x2 u, u, v, w;\n\tmov.b64 {%0, %1}, u;\n\t}"
+      : "+f"(x), "+f"(y) : "f"(f), "f"(a), "f"(b));
+}
+__device__ __forceinline__ void add4(float (&x)[4], const float (&t)[4]) {
+  const float2 u = ptx::add2(make_float2(x[0], x[1]), make_float2(t[0], t[1])), v = ptx::add2(make_float2(x[2], x[3]), make_float2(t[2], t[3]));
+  x[0] = u.x; x[1] = u.y; x[2] = v.x; x[3] = v.y;
+}
+// A 16 x 16 tile of the product of split operands: the smallest terms first, in
+// accumulators of its own.  The tensor cores cut a sum off rather than round it, every time and at the size of what it
+// has come to, so long sums are made of these tiles by ordinary additions (states: 2.4e-6 relative to 64 bits with the sum
+// in the tensor cores' accumulators, fp32 outputs 1.4e-6 to 4e-6; see the tests for what is left).
+template <int NA, int NB>
+__device__ __forceinline__ void tile_product(float (&t0)[4], float (&t1)[4], const uint32_t (&a)[NA][4], const uint32_t (&y)[NB][4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) t0[i] = t1[i] = 0.f;
+#pragma unroll
+  for (int order = NA - 1; order >= 0; --order) {
+#pragma unroll
+    for (int pb = NB - 1; pb >= 0; --pb) {
+      const int pa = order - pb;
+      if (pa < 0) continue;
+      mma(t0, a[pa], y[pb][0], y[pb][1]);
+      mma(t1, a[pa], y[pb][2], y[pb][3]);
+    }
+  }
+}
+
 template <typename T, int D> struct LaCfg {
   static constexpr int NP = sizeof(T) == 2 ? 1 : 3;            // bf16 terms of an element
-  static constexpr int NA = sizeof(T) == 2 ? 2 : 3;            // of a decayed key
   static constexpr int C = (NP == 3 && D == 128) ? 32 : 64;    // tokens of a chunk (fp32, d = 128: by shared memory)
   static constexpr int NW = D == 128 ? 8 : 4, NTS = NW * 32, NT = 2 * NTS;      // warps of the state, and as many of the outputs
   static constexpr int RW = C / 16, CW = NW / RW, OC = D / CW; // warps over rows and over columns of the output tile
@@ -88,7 +116,7 @@ template <typename T, int D> struct LaCfg {
   static constexpr int SLOTS = NP == 1 ? 8 : 4;                // keys and values of two pairs of chunks, or of one
   static constexpr int OFF_S = STAGES * 3 * OPER, OFF_W = SLOTS * OPER > OFF_S + SBUF * STATE ? SLOTS * OPER : OFF_S + SBUF * STATE;
   static constexpr int OFF_K = OFF_W + (C + 4) * 4;            // the keys' weights
-  static constexpr size_t SMEM = OFF_K + 2 * C * sizeof(float);
+  static constexpr size_t SMEM = OFF_K + 2 * C * 4;
   static constexpr int PER_SM = D == 32 && NP == 1 ? 3 : D < 128 ? 2 : 1;
   static_assert(PER_SM * (SMEM + 1024) <= 228 * 1024, "shared memory");
   static_assert(STAGES * 3 * OPER >= D * D * 4, "the segments' states lie over the tiles");
@@ -98,7 +126,7 @@ template <typename T, int D>
 __global__ void __launch_bounds__(LaCfg<T, D>::NT, LaCfg<T, D>::PER_SM)
 linear_attention_kernel(const __grid_constant__ LinearParams prm) {
   using F = LaCfg<T, D>;
-  constexpr int C = F::C, NP = F::NP, NA = F::NA, NT = F::NT, PITCH = F::PITCH;
+  constexpr int C = F::C, NP = F::NP, NT = F::NT, PITCH = F::PITCH;
   extern __shared__ __align__(16) uint8_t smem[];
   const uint32_t sbase = ptx::smem_u32(smem);
   float* sw = reinterpret_cast<float*>(smem + F::OFF_W);       // g^0 .. g^C
@@ -202,15 +230,28 @@ linear_attention_kernel(const __grid_constant__ LinearParams prm) {
   for (int n = 0; n < F::SC / 8; ++n)
 #pragma unroll
     for (int i = 0; i < 4; ++i) st[n][i] = 0.f;
-  auto update = [&](uint32_t sk, uint32_t sv, int n_real) {
+  // bf16 storage: three terms of a decayed key, and sums outside of the state's accumulators (of the chunk, d = 128: of
+  // 16 events, by registers), go in where they count, in the state that is returned.  A chunk whose last event has
+  // decayed to less than 2^-3 by then gets two terms straight into the accumulators (2.4e-6 of the sum, an eighth of
+  // that in the state), as all do where no state is returned.
+  auto update_as = [&](uint32_t sk, uint32_t sv, int n_real, auto kind) {
+    constexpr int TERMS = decltype(kind)::value;
+    constexpr bool NEAR = NP == 1 && TERMS == 3 && D < 128, EXACT = NP == 3 || (TERMS == 3 && D == 128);
     const float gn = sw[n_real];
+    float t[NEAR ? F::SC / 8 : 1][4];   // bf16, the chunk's own sum
+    if constexpr (NEAR) {
 #pragma unroll
-    for (int n = 0; n < F::SC / 8; ++n) { mul2(st[n][0], st[n][1], gn); mul2(st[n][2], st[n][3], gn); }
+      for (auto& x : t) x[0] = x[1] = x[2] = x[3] = 0.f;
+    }
+    if constexpr (!NEAR) {
+#pragma unroll
+      for (int n = 0; n < F::SC / 8; ++n) { mul2(st[n][0], st[n][1], gn); mul2(st[n][2], st[n][3], gn); }
+    }
     const float* wk = swk + (C - n_real) + 2 * j;
-#pragma unroll
-    for (int ks = 0; ks < C / 16; ++ks) {
+#pragma unroll(EXACT || D == 128 ? 1 : C / 16)
+    for (int ks = 0; ks < C / 16; ++ks) {          // (one after the other where registers are short)
       const float w[4] = {wk[ks * 16], wk[ks * 16 + 1], wk[ks * 16 + 8], wk[ks * 16 + 9]};   // of tokens 2j, 2j+1, 2j+8, 2j+9
-      uint32_t a[NA][4];
+      uint32_t a[TERMS][4];
       {
         uint32_t x[NP][4];
 #pragma unroll
@@ -220,27 +261,52 @@ linear_attention_kernel(const __grid_constant__ LinearParams prm) {
           float u = lo_f(x[NP - 1][i]), v = hi_f(x[NP - 1][i]);
 #pragma unroll
           for (int p = NP - 2; p >= 0; --p) { u += lo_f(x[p][i]); v += hi_f(x[p][i]); }
-          uint32_t y[NA];
-          split<NA>(u * w[(i >> 1) * 2], v * w[(i >> 1) * 2 + 1], y);
+          uint32_t y[TERMS];
+          split<TERMS>(u * w[(i >> 1) * 2], v * w[(i >> 1) * 2 + 1], y);
 #pragma unroll
-          for (int p = 0; p < NA; ++p) a[p][i] = y[p];
+          for (int p = 0; p < TERMS; ++p) a[p][i] = y[p];
         }
       }
+      if constexpr (EXACT) {
 #pragma unroll
-      for (int pb = 0; pb < NP; ++pb) {
+        for (int n2 = 0; n2 < F::SC / 16; ++n2) {
+          uint32_t y[NP][4];
+          float t[2][4];
+#pragma unroll
+          for (int pb = 0; pb < NP; ++pb) ldsm_t(y[pb], sv + pb * F::TILE + ks * 16 * PITCH + (nh * F::SC + n2 * 16) * 2 + off_nm);
+          tile_product<TERMS, NP>(t[0], t[1], a, y);
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            add4(st[2 * n2 + x], t[x]);
+          }
+        }
+      } else {
         uint32_t y[F::SC / 16][4];
 #pragma unroll
-        for (int n2 = 0; n2 < F::SC / 16; ++n2)
-          ldsm_t(y[n2], sv + pb * F::TILE + ks * 16 * PITCH + (nh * F::SC + n2 * 16) * 2 + off_nm);
+        for (int n2 = 0; n2 < F::SC / 16; ++n2) ldsm_t(y[n2], sv + ks * 16 * PITCH + (nh * F::SC + n2 * 16) * 2 + off_nm);
 #pragma unroll
-        for (int pa = 0; pa < NA - pb; ++pa)       // (an accumulator's next product is SC / 8 products away)
+        for (int pa = TERMS - 1; pa >= 0; --pa)    // (an accumulator's next product is SC / 8 products away)
 #pragma unroll
           for (int n2 = 0; n2 < F::SC / 16; ++n2) {
-            mma(st[2 * n2], a[pa], y[n2][0], y[n2][1]);
-            mma(st[2 * n2 + 1], a[pa], y[n2][2], y[n2][3]);
+            mma(NEAR ? t[NEAR ? 2 * n2 : 0] : st[2 * n2], a[pa], y[n2][0], y[n2][1]);
+            mma(NEAR ? t[NEAR ? 2 * n2 + 1 : 0] : st[2 * n2 + 1], a[pa], y[n2][2], y[n2][3]);
           }
       }
     }
+    if constexpr (NEAR) {
+#pragma unroll
+      for (int n = 0; n < F::SC / 8; ++n) { fma2(st[n][0], st[n][1], gn, t[n][0], t[n][1]); fma2(st[n][2], st[n][3], gn, t[n][2], t[n][3]); }
+    }
+  };
+  auto update = [&](uint32_t sk, uint32_t sv, int c) {
+    const int n_real = min(C, len - c * C);
+    if constexpr (NP == 1) {
+      if (R.s1 == nullptr || (float)max(len - (c + 1) * C, 1) * l2 < -3.f) {
+        update_as(sk, sv, n_real, std::integral_constant<int, 2>{});
+        return;
+      }
+    }
+    update_as(sk, sv, n_real, std::integral_constant<int, 3>{});
   };
 
   // ---- the segment's own state, where somebody needs it: both kinds of warps, a chunk of a pair each ------------
@@ -271,7 +337,7 @@ linear_attention_kernel(const __grid_constant__ LinearParams prm) {
       const int at = (c0 + 2 * pair) * C, n0 = min(C, len - at), n1 = c0 + 2 * pair + 1 < c1 ? min(C, len - at - C) : 0;
       if (!state_warp) fade(sw[n0]);
       const int mine = state_warp ? n0 : n1;
-      if (mine > 0) update(slot(pair, state_warp ? 0 : 1, 0), slot(pair, state_warp ? 0 : 1, 1), mine);
+      if (mine > 0) update(slot(pair, state_warp ? 0 : 1, 0), slot(pair, state_warp ? 0 : 1, 1), c0 + 2 * pair + (state_warp ? 0 : 1));
       if (state_warp) fade(sw[n1]);
       if (NP != 1) all();
     }
@@ -342,7 +408,7 @@ linear_attention_kernel(const __grid_constant__ LinearParams prm) {
     start(c0);
     for (int c = c0; c < c1; ++c) {
       const int stage = before(c);
-      update(oper(stage, 1), oper(stage, 2), min(C, len - c * C));
+      update(oper(stage, 1), oper(stage, 2), c);
       after();
       if (c + 1 < c1) put_state(F::SBUF == 2 ? (c + 1 - c0) & 1 : 0);
     }
@@ -378,27 +444,36 @@ linear_attention_kernel(const __grid_constant__ LinearParams prm) {
       for (int n = 0; n < F::OC / 8; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[n][i] = 0.f;
-      uint32_t q[NP][D / 16][4];
+      uint32_t q[NP == 1 ? D / 16 : 1][4];           // (three terms: read where they are used)
+      auto query = [&](int ks, uint32_t (&x)[NP][4]) {
 #pragma unroll
-      for (int p = 0; p < NP; ++p)
+        for (int p = 0; p < NP; ++p) ldsm(x[p], sq + p * F::TILE + rw * 16 * PITCH + ks * 32 + off_nm);
+      };
+      if constexpr (NP == 1) {
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) ldsm(q[p][ks], sq + p * F::TILE + rw * 16 * PITCH + ks * 32 + off_nm);
+        for (int ks = 0; ks < D / 16; ++ks) ldsm(q[ks], sq + rw * 16 * PITCH + ks * 32 + off_nm);
+      }
       // q S, then its rows' powers
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks)
+      for (int ks = 0; ks < D / 16; ++ks) {
+        uint32_t qa[NP][4];
+        if constexpr (NP != 1) query(ks, qa);
 #pragma unroll
-        for (int n2 = 0; n2 < F::OC / 16; ++n2)
+        for (int n2 = 0; n2 < F::OC / 16; ++n2) {
+          uint32_t y[NP][4];
 #pragma unroll
-          for (int pb = 0; pb < NP; ++pb) {
-            uint32_t y[4];
-            ldsm_t(y, ss + pb * D * PITCH + ks * 16 * PITCH + (cw * F::OC + n2 * 16) * 2 + off_nm);
-#pragma unroll
-            for (int pa = 0; pa < NP; ++pa)
-              if (pa + pb < NP) {
-                mma(o[2 * n2], q[pa][ks], y[0], y[1]);
-                mma(o[2 * n2 + 1], q[pa][ks], y[2], y[3]);
-              }
+          for (int pb = 0; pb < NP; ++pb) ldsm_t(y[pb], ss + pb * D * PITCH + ks * 16 * PITCH + (cw * F::OC + n2 * 16) * 2 + off_nm);
+          if constexpr (NP == 1) {
+            mma(o[2 * n2], q[ks], y[0][0], y[0][1]);
+            mma(o[2 * n2 + 1], q[ks], y[0][2], y[0][3]);
+          } else {
+            float t[2][4];
+            tile_product<NP, NP>(t[0], t[1], qa, y);
+            add4(o[2 * n2], t[0]);
+            add4(o[2 * n2 + 1], t[1]);
           }
+        }
+      }
       const int t0 = rw * 16 + g, t1 = t0 + 8;
       {
         const float f0 = R.aq * sw[t0 + 1 - rev], f1 = R.aq * sw[t1 + 1 - rev];
@@ -421,8 +496,8 @@ linear_attention_kernel(const __grid_constant__ LinearParams prm) {
             for (int kt = 0; kt < KT; ++kt) {
               uint32_t y[4];
               ldsm(y, sk + kt * 16 * PITCH + ks * 32 + off_mn);
-              mma(z[kt][0], q[0][ks], y[0], y[1]);
-              mma(z[kt][1], q[0][ks], y[2], y[3]);
+              mma(z[kt][0], q[ks], y[0], y[1]);
+              mma(z[kt][1], q[ks], y[2], y[3]);
             }
 #pragma unroll
           for (int kt = 0; kt < KT; ++kt) {
@@ -455,25 +530,17 @@ linear_attention_kernel(const __grid_constant__ LinearParams prm) {
 #pragma unroll
       for (int kt = 0; kt < C / 16; ++kt) {
         if (kt > rw) break;
-        float p0[4], p1[4];
-        {
-          float z[2][2][4];                          // two chains for each half of the keys
+        float p0[4] = {0.f, 0.f, 0.f, 0.f}, p1[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) z[0][0][i] = z[0][1][i] = z[1][0][i] = z[1][1][i] = 0.f;
+        for (int ks = 0; ks < D / 16; ++ks) {
+          uint32_t qa[NP][4], y[NP][4];
+          float t[2][4];
+          query(ks, qa);
 #pragma unroll
-          for (int ks = 0; ks < D / 16; ++ks)
-#pragma unroll
-            for (int pb = 0; pb < NP; ++pb) {
-              uint32_t y[4];
-              ldsm(y, sk + pb * F::TILE + kt * 16 * PITCH + ks * 32 + off_mn);
-#pragma unroll
-              for (int pa = 0; pa < NP - pb; ++pa) {
-                mma(z[(ks + pa) & 1][0], q[pa][ks], y[0], y[1]);
-                mma(z[(ks + pa) & 1][1], q[pa][ks], y[2], y[3]);
-              }
-            }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) { p0[i] = z[0][0][i] + z[1][0][i]; p1[i] = z[0][1][i] + z[1][1][i]; }
+          for (int pb = 0; pb < NP; ++pb) ldsm(y[pb], sk + pb * F::TILE + kt * 16 * PITCH + ks * 32 + off_mn);
+          tile_product<NP, NP>(t[0], t[1], qa, y);
+          add4(p0, t[0]);
+          add4(p1, t[1]);
         }
         if (kt == rw) {
 #pragma unroll
@@ -500,18 +567,15 @@ linear_attention_kernel(const __grid_constant__ LinearParams prm) {
           for (int p = 0; p < NP; ++p) a[p][3] = y[p];
         }
 #pragma unroll
-        for (int n2 = 0; n2 < F::OC / 16; ++n2)
+        for (int n2 = 0; n2 < F::OC / 16; ++n2) {
+          uint32_t y[NP][4];
+          float t[2][4];
 #pragma unroll
-          for (int pb = 0; pb < NP; ++pb) {
-            uint32_t y[4];
-            ldsm_t(y, sv + pb * F::TILE + kt * 16 * PITCH + (cw * F::OC + n2 * 16) * 2 + off_nm);
-#pragma unroll
-            for (int pa = 0; pa < NP; ++pa)
-              if (pa + pb < NP) {
-                mma(o[2 * n2], a[pa], y[0], y[1]);
-                mma(o[2 * n2 + 1], a[pa], y[2], y[3]);
-              }
-          }
+          for (int pb = 0; pb < NP; ++pb) ldsm_t(y[pb], sv + pb * F::TILE + kt * 16 * PITCH + (cw * F::OC + n2 * 16) * 2 + off_nm);
+          tile_product<NP, NP>(t[0], t[1], a, y);
+          add4(o[2 * n2], t[0]);
+          add4(o[2 * n2 + 1], t[1]);
+        }
       }
       }
 #pragma unroll
