@@ -384,7 +384,8 @@ solar_status_t solar_lowrank_factor_static(int B, int M, int N, int d, int r, so
  * fp32.  bf16 storage: the decayed scores and the state as an operand of q S are rounded to bf16 (the returned state is not).
  * An input that is not finite makes the outputs of its user and head infinite or NaN from there on, and can do so for
  * up to 15 events before it.
- * H <= 21845; T = 0 copies state0 to state.
+ * An output may not overlap an input or another output (the same address is refused).
+ * H <= 21845; T <= 2^30; T = 0 copies state0 to state.
  * ------------------------------------------------------------------------- */
 solar_status_t solar_linear_attention_fwd(int B, int T, int H, int d, solar_dtype_t dt,
                                           const void* Q, const long long* q_strides,
@@ -423,7 +424,7 @@ solar_status_t solar_linear_attention_step(int B, int H, int d, solar_dtype_t dt
  * The cache of B users, H heads and N rows a head (N a multiple of SOLAR_CACHE_BLOCK = 64):
  *   k8, v8            [B,H,N,d]    e4m3
  *   k_scale, v_scale  [B,H,N/64]   f32   one scale per block of 64 rows: a row is its bytes times the scale of its block
- * The append writes powers of two: the smallest 2^e, e >= -100, with max|x| <= 448 * 2^e over the block's rows.
+ * Scales are positive.  The append writes powers of two: the smallest 2^e, e >= -100, with max|x| <= 448 * 2^e over the block's rows.
  * Rows that were never written are never read as numbers; the cache needs no initial value.
  *
  * solar_history_cache_append: rows t = 0 .. counts[b] - 1 of K, V [B,T,H,d] dt become rows start[b] + t of user b,
@@ -445,7 +446,7 @@ solar_status_t solar_linear_attention_step(int B, int H, int d, solar_dtype_t dt
  * Token tensors have strides as in solar_linear_attention_fwd.  One launch each, no workspace; results are
  * reproducible bit for bit.  Sums and the softmax's statistics are fp32; the weights of the softmax enter their
  * product with V as fp16 of 2^15 times their value relative to the largest (fp32 storage: two fp16 halves).
- * H <= 21845; N <= 2^30.
+ * H <= 21845; T, M, N <= 2^30.
  * ------------------------------------------------------------------------- */
 #define SOLAR_CACHE_BLOCK 64
 enum { SOLAR_FLAG_CAUSAL = 2 };

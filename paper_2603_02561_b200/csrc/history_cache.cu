@@ -551,7 +551,8 @@ history_attention_kernel(LinearOperand q, T* O, long long ob, long long ot, long
 template <typename T, int D>
 cudaError_t launch_append_td(int B, int T_new, int H, int N, const LinearOperand& k, const LinearOperand& v, const int* start,
                              const int* counts, uint8_t* k8, uint8_t* v8, float* k_scale, float* v_scale, cudaStream_t st) {
-  const dim3 grid((T_new + kBlock - 2) / kBlock + 1, 2 * H, B);
+  const int most = T_new < N ? T_new : N;          // rows past the capacity touch nothing
+  const dim3 grid((most + kBlock - 2) / kBlock + 1, 2 * H, B);
   return launch_pdl(history_append_kernel<T, D>, grid, dim3(D == 32 ? 128 : 256), 0, st, k, v, T_new, N, start, counts, k8, v8, k_scale, v_scale);
 }
 
@@ -570,9 +571,12 @@ cudaError_t launch_attention_td(const HistoryCall& c, cudaStream_t st) {
     if (w != cudaSuccess) return w;
     if (dev < kMaxDevicesCached) wide[dev] = true;
   }
-  // the rows are split while the CTAs still run at once and each warp has a block to itself
+  // The rows are split while the CTAs still run at once and each warp has a block.  Clusters of sixteen only where half
+  // of the GPU's CTAs are enough: they need sixteen SMs of one group at the same time (256 queries of one user over
+  // 10240 x 128: 31 us in sixteens, 21 in eights).
+  const long long room = (long long)kNumSMs * kPerSm<T, D>;
   int splits = 1;
-  while (splits < kMaxSplits && ctas * splits * 2 <= (long long)kNumSMs * kPerSm<T, D> && c.N / kBlock >= splits * 2 * kWarps) splits *= 2;
+  while (splits < kMaxSplits && ctas * splits * 2 <= (splits == 8 ? room / 2 : room) && c.N / kBlock >= splits * 2 * kWarps) splits *= 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(tiles * splits), c.H, c.B);
   cfg.blockDim = dim3(kWarps * 32);

@@ -185,8 +185,9 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
       ks = held ? ld_dep(ksc + blk) : 1.f;
       vs = held ? ld_dep(vsc + blk) : 1.f;
     };
+    int issued = 0;
     if (ct == 0)
-      for (int t = 0; t < min(nt, kStages); ++t) copy(t);
+      for (; issued < min(nt, kStages); ++issued) copy(issued);
     if (nt > 0) scales(0);
     for (int t = 0; t < nt; ++t) {
       const int st = t % kStages, first = (t0 + t) * NTOK;
@@ -222,14 +223,14 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
         s_scale[st][ct] = make_float4(ks, lv, exp2f(-lv - kLift), 0.f);
       }
       asm volatile("bar.sync 1, %0;" ::"n"(kConvThreads) : "memory");
-      if (ct == 0 && t + kStages < nt) copy(t + kStages);       // everybody has read the tile's bytes
+      if (ct == 0 && issued < nt && *err == 0) copy(issued++);  // everybody has read the tile's bytes
       if (t + 1 < nt) scales(t + 1);
       if (odd) s_odd[st] = 1;
       ptx::fence_proxy_async_smem();
       ptx::mbar_arrive_warp(&kv_full[st], lane);
     }
     if (ct == 0 && *err != 0)                      // a wait ran out: the copies land before the CTA leaves
-      for (int t = max(0, nt - kStages); t < nt; ++t) {
+      for (int t = max(0, issued - kStages); t < issued; ++t) {
         int dummy = 0;
         ptx::mbar_wait(&raw_full[t % kStages], (t / kStages) & 1, &dummy, 0);
       }
@@ -469,15 +470,22 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
   }
 }
 
+// One CTA per SM: the cache's rows are split while all CTAs still run at once (in clusters fewer do), four tiles at least
+// to each.
+int flash_splits(long long ctas, int tiles) {
+  constexpr int kAtOnce[] = {0, 0, kNumSMs, 0, 132, 0, 0, 0, 112};
+  int splits = 1;
+  while (splits < kMaxSplits && ctas * splits * 2 <= kAtOnce[splits * 2] && tiles >= splits * 2 * 4) splits *= 2;
+  return splits;
+}
+
 template <int D> cudaError_t launch_d(const HistoryCall& c, cudaStream_t st) {
   using F = HfCfg<D>;
   static bool limits_set[kMaxDevicesCached] = {};
   const cudaError_t e = set_kernel_limits(reinterpret_cast<const void*>(&history_flash_kernel<D>), F::SMEM, limits_set);
   if (e != cudaSuccess) return e;
-  const long long tiles = ((long long)c.M * c.G + kRows - 1) / kRows, ctas = tiles * c.H * c.B;
-  // one CTA per SM: the rows are split while all of them still run at once, four tiles at least to each
-  int splits = 1;
-  while (splits < kMaxSplits && ctas * splits * 2 <= kNumSMs && c.N >= splits * 2 * 4 * F::NTOK) splits *= 2;
+  const long long tiles = ((long long)c.M * c.G + kRows - 1) / kRows;
+  const int splits = flash_splits(tiles * c.H * c.B, (c.N + F::NTOK - 1) / F::NTOK);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(tiles * splits), c.H, c.B);
   cfg.blockDim = dim3(kThreads);
@@ -495,8 +503,21 @@ template <int D> cudaError_t launch_d(const HistoryCall& c, cudaStream_t st) {
 
 }  // namespace
 
+// Which of the two kernels a call gets: the one with the shorter estimate.  This one works on 256 rows at a time, 2.2 us a
+// tile of 128 cache rows (d = 128: 1.5 us, 64 rows) wherever a CTA runs, and about 14 us to start and end; the other takes
+// 1.35 ns (2.5 ns) of the GPU for 16 rows and 64 cache rows, and 6 us.  us a call, measured, the other kernel and this one:
+//   d = 64    1 x 512 queries, 10240 rows      13 and 37      16 x 256, 10240    57 and 56     16 x 512, 10240   111 and 57
+//             64 x 128, 2048                   29 and 29      64 x 256, 2048     46 and 32     16 x 512, 256      11 and 14
+//   d = 128   16 x 128, 10240                  57 and 69      16 x 192, 10240   106 and 73     64 x 128, 2048     53 and 39
 bool history_flash_supported(int d, solar_dtype_t dt, const HistoryCall& c) {
-  return dt == SOLAR_BF16 && (d == 64 || d == 128) && (long long)c.M * c.G >= 96;
+  if (dt != SOLAR_BF16 || (d != 64 && d != 128)) return false;
+  const int per_tile = d == 64 ? HfCfg<64>::NTOK : HfCfg<128>::NTOK;
+  const long long heads = (long long)c.H * c.B, rows = (long long)c.M * c.G;
+  const long long ctas = (rows + kRows - 1) / kRows * heads;
+  const int tiles = (c.N + per_tile - 1) / per_tile, splits = flash_splits(ctas, tiles);
+  const double here = 14. + (double)((ctas * splits + kNumSMs - 1) / kNumSMs) * ((tiles + splits - 1) / splits) * (d == 64 ? 2.2 : 1.5);
+  const double other = 6. + (double)((rows + 15) / 16) * heads * (c.N / kBlock) * (d == 64 ? 1.35e-3 : 2.5e-3);
+  return here < other;
 }
 cudaError_t launch_history_flash(int d, const HistoryCall& c, cudaStream_t st) {
   return d == 64 ? launch_d<64>(c, st) : launch_d<128>(c, st);

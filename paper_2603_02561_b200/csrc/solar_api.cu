@@ -113,7 +113,7 @@ solar_status_t check_linear(int B, int T, int H, int d, solar_dtype_t dt) {
   if (dt != SOLAR_F32 && dt != SOLAR_BF16) return SOLAR_ERR_UNSUPPORTED;
   if (B < 0 || T < 0 || H < 1) return SOLAR_ERR_INVALID_ARG;
   if (d != 32 && d != 64 && d != 128) return SOLAR_ERR_UNSUPPORTED;
-  if (B > 65535 || H > 65535 / 3) return SOLAR_ERR_UNSUPPORTED;
+  if (B > 65535 || H > 65535 / 3 || T > (1 << 30)) return SOLAR_ERR_UNSUPPORTED;
   return SOLAR_OK;
 }
 solar_status_t check_cache(int N) {
@@ -426,6 +426,7 @@ solar_status_t solar_linear_attention_fwd(int B, int T, int H, int d, solar_dtyp
     SOLAR_TRY(token_input(B, T, H, d, dt, V, v_strides, &r.v));
     Tokens o;
     SOLAR_TRY(token_output(B, T, H, d, dt, O, o_strides, &o));
+    if (O == Q || O == K || O == V) return SOLAR_ERR_INVALID_ARG;              // other CTAs still read them
     r.o = O; r.ob = o.sb; r.ot = o.st; r.oh = o.sh;
   }
   SOLAR_TRY(check_word_ptr(log_decay));
@@ -457,6 +458,9 @@ solar_status_t solar_linear_attention_bwd(int B, int T, int H, int d, solar_dtyp
     SOLAR_TRY(token_output(B, T, H, d, dt, dQ, dq_strides, &out[0]));
     SOLAR_TRY(token_output(B, T, H, d, dt, dK, dk_strides, &out[1]));
     SOLAR_TRY(token_output(B, T, H, d, dt, dV, dv_strides, &out[2]));
+    const void* made[3] = {dQ, dK, dV};
+    for (int i = 0; i < 3; ++i)
+      if (made[i] == Q || made[i] == K || made[i] == V || made[i] == dO || made[i] == made[(i + 1) % 3]) return SOLAR_ERR_INVALID_ARG;
   }
   SOLAR_TRY(check_word_ptr(log_decay));
   SOLAR_TRY(check_optional(lengths, 4));
@@ -497,6 +501,7 @@ solar_status_t solar_linear_attention_step(int B, int H, int d, solar_dtype_t dt
   Tokens o;
   const long long s[3] = {o_strides ? o_strides[0] : 0, 0, o_strides ? o_strides[1] : 0};
   SOLAR_TRY(token_output(B, 1, H, d, dt, O, o_strides ? s : nullptr, &o));
+  if (O == Q || O == K || O == V) return SOLAR_ERR_INVALID_ARG;
   SOLAR_TRY(check_word_ptr(log_decay));
   SOLAR_TRY(check_ptr(state));
   return from_cuda(launch_linear_step(B, H, d, dt, op[0], op[1], op[2], log_decay, scale, state, O, o.sb, o.sh,

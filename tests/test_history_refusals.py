@@ -9,6 +9,7 @@ from paper_2603_02561_b200 import build as solar_build
 from paper_2603_02561_b200 import solar
 
 P, vp = ctypes.c_void_p(0x1000), ctypes.c_void_p
+P2, P3, P4 = (ctypes.c_void_p(0x2000 + 0x1000 * i) for i in range(3))          # outputs
 S3 = lambda *x: (ctypes.c_longlong * 3)(*x)  # noqa: E731
 BF, F32, I32 = torch.bfloat16, torch.float32, torch.int32
 INVALID, UNSUPPORTED = solar.ERR_INVALID_ARG, solar.ERR_UNSUPPORTED
@@ -20,16 +21,16 @@ def L():
     return solar.lib()
 
 
-def fwd(L, B=2, T=5, H=3, d=64, dt=1, Q=P, qs=None, K=P, V=P, ld=P, lengths=None, s0=None, O=P, os=None, S=P):
+def fwd(L, B=2, T=5, H=3, d=64, dt=1, Q=P, qs=None, K=P, V=P, ld=P, lengths=None, s0=None, O=P2, os=None, S=P):
     return L.solar_linear_attention_fwd(B, T, H, d, dt, Q, qs, K, None, V, None, ld, 0.1, lengths, s0, O, os, S, None)
 
 
-def bwd(L, B=2, T=5, H=3, d=64, dt=1, dO=P, s0=None, ds=None, dQ=P, dqs=None, dK=P, dV=P, d0=None):
+def bwd(L, B=2, T=5, H=3, d=64, dt=1, dO=P, s0=None, ds=None, dQ=P2, dqs=None, dK=P3, dV=P4, d0=None):
     return L.solar_linear_attention_bwd(B, T, H, d, dt, P, None, P, None, P, None, P, 0.1, None, s0, dO, None, ds, dQ, dqs, dK, None, dV,
                                         None, d0, None)
 
 
-def step(L, B=2, H=3, d=64, dt=1, Q=P, ld=P, S=P, O=P, os=None):
+def step(L, B=2, H=3, d=64, dt=1, Q=P, ld=P, S=P, O=P2, os=None):
     return L.solar_linear_attention_step(B, H, d, dt, Q, None, P, None, P, None, ld, 0.1, S, O, os, None)
 
 
@@ -69,6 +70,19 @@ def test_pointers(L):
 def test_a_state_is_not_read_and_written_in_one_call(L):
     assert fwd(L, s0=P, S=P) == INVALID
     assert bwd(L, ds=P, d0=P) == INVALID and bwd(L, s0=P, d0=P) == INVALID
+
+
+def test_outputs_over_inputs_and_over_one_another(L):
+    assert fwd(L, O=P) == INVALID and step(L, O=P) == INVALID
+    for n in ("dQ", "dK", "dV"):
+        assert bwd(L, **{n: P}) == INVALID
+    assert bwd(L, dQ=P3) == INVALID and bwd(L, dQ=P4) == INVALID and bwd(L, dK=P4) == INVALID
+
+
+def test_lengths_past_what_is_counted(L):
+    for call in (fwd, bwd, append):
+        assert call(L, T=(1 << 30) + 1) == UNSUPPORTED
+    assert attend(L, M=(1 << 30) + 1) == UNSUPPORTED
 
 
 def test_strides(L):
