@@ -438,7 +438,9 @@ solar_status_t solar_linear_attention_step(int B, int H, int d, solar_dtype_t dt
  *   Q        [B,M,Hq,d] dt (in)   Hq a multiple of H: query head i reads cached head i / (Hq / H)
  *   lengths  [B] int       (in)   taken as 0 .. N
  *   flags                  (in)   SOLAR_FLAG_CAUSAL: the M queries are the last M rows, query m sees rows
- *                                 0 .. lengths[b] - M + m
+ *                                 0 .. lengths[b] - M + m (of those that the cache has).  Queries that are padded behind a
+ *                                 user's own, as K and V were for the append: lengths[b] = start[b] + M, whatever
+ *                                 counts[b] is; the user's queries then see what is theirs, the padding's are anything.
  *   O        [B,M,Hq,d] dt (out)  zeros for a query that sees no row
  * A query that sees a row of K or V that is not finite comes out NaN (in the components of that row of V at least);
  * what it does not see does not reach it.

@@ -221,7 +221,7 @@ history_attention_kernel(LinearOperand q, T* O, long long ob, long long ot, long
   const long long rows = (long long)M * G;
 
   pdl_wait();
-  const int len = min(max(ld_dep(lengths + b), 0), N);
+  const int told = ld_dep(lengths + b), len = min(max(told, 0), N);
   // the row of lane group g, and the one eight below: queries r / G, head r % G of the group
   long long row[2];
   int limit[2];                                    // cached rows that it sees
@@ -233,7 +233,7 @@ history_attention_kernel(LinearOperand q, T* O, long long ob, long long ot, long
     const bool real = row[i] < rows;
     const long long mq = real ? row[i] / G : 0;
     const int hq = real ? (int)(row[i] - mq * G) : 0;
-    limit[i] = real && causal ? (int)max(min((long long)len, len - M + mq + 1), 0ll) : len;
+    limit[i] = real && causal ? (int)max(min((long long)len, (long long)told - M + mq + 1), 0ll) : len;
     const T* p = static_cast<const T*>(q.p) + (long long)b * q.sb + mq * q.st + (long long)(hk * G + hq) * q.sh;
     float x[KS][4], top = 0.f;
 #pragma unroll
@@ -268,7 +268,7 @@ history_attention_kernel(LinearOperand q, T* O, long long ob, long long ot, long
   int reach = len;
   if (causal) {
     const long long last = min((long long)(rt + 1) * kRowsPerCta, rows) - 1;
-    reach = (int)max(min((long long)len, len - M + last / G + 1), 0ll);
+    reach = (int)max(min((long long)len, (long long)told - M + last / G + 1), 0ll);
   }
   const int blocks = (reach + kBlock - 1) / kBlock, per = (blocks + splits - 1) / splits;
   const int b0 = min(split * per, blocks), b1 = min(b0 + per, blocks);

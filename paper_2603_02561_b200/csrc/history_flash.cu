@@ -106,10 +106,10 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
   }
   if (warp == kMmaWarp) ptx::tmem_alloc(&s_tmem, 512);
   pdl_wait();
-  const int len = min(max(ld_dep(c.lengths + b), 0), c.N);
+  const int told = ld_dep(c.lengths + b), len = min(max(told, 0), c.N);
   auto limit_of = [&](long long row) {             // cache rows that a query row sees
     if (!c.causal) return len;
-    return (int)max(min((long long)len, len - c.M + row / c.G + 1), 0ll);
+    return (int)max(min((long long)len, (long long)told - c.M + row / c.G + 1), 0ll);
   };
   const int reach = limit_of(min(row0 + kRows, rows) - 1), least = limit_of(row0);
   const int all = (reach + NTOK - 1) / NTOK, per = (all + splits - 1) / splits;

@@ -588,7 +588,7 @@ def history_cache_append(k, v, cache, start, counts=None, stream=None):
 
 def history_cache_attention(q, cache, lengths, scale, flags=0, O=None, stream=None):
     """solar_history_cache_attention: q [B,M,Hq,d] over the first lengths[b] rows of `cache` -> O [B,M,Hq,d].
-    FLAG_CAUSAL: the queries are the last M rows."""
+    FLAG_CAUSAL: the queries are the last M rows (a padded batch: lengths = start + M)."""
     dt, dev, shape = q.dtype, _device_of(q, "q", 4), q.shape
     B, H, N, d = _cache_sizes(cache, dev)
     M, Hq = shape[1], shape[2]

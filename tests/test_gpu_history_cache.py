@@ -38,7 +38,7 @@ def near(got, q, c, lengths, scale, causal, dt):
     want, size = ho.attention(f64(q), k8, v8, ks, vs, lengths, scale, causal)
     got = f64(got)
     assert np.isfinite(got).all()
-    top = np.abs(k8 * np.repeat(ks, 64, axis=2)[..., None]).max() * np.abs(f64(q)).sum(-1).max() * abs(scale)
+    top = np.nanmax(np.abs(k8 * np.repeat(ks, 64, axis=2)[..., None])) * np.abs(f64(q)).sum(-1).max() * abs(scale)
     dz = 2 * top * 2.0 ** -20
     out, rest = (2.0 ** -8, 2.0 ** -10 + 2.0 ** -14) if dt is BF else (2.0 ** -24, 2.0 ** -20 + 2.0 ** -16)
     err = np.abs(got - want)
@@ -166,6 +166,24 @@ def test_a_row_that_is_not_finite_reaches_only_those_that_see_it(dt, d, what):
     got = solar.history_cache_attention(q, c, lengths, 0.1, flags=solar.FLAG_CAUSAL)
     assert torch.isnan(got[0, 150:, 0, 7]).all()
     assert torch.equal(got[0, :150], want[0, :150])
+
+
+@pytest.mark.parametrize("dt,d,T", [(BF, 64, 40), (BF, 64, 400), (BF, 128, 400), (F32, 32, 40)])
+def test_a_padded_batch_of_new_histories(dt, d, T):
+    """Queries padded as the appended rows were, the cache behind those rows never written, one user's padding past its end."""
+    B, H, Hq, N = 3, 2, 4, 512
+    start, counts = [10, 120, 0], [T, min(13, T), 0]
+    c = filled(B, H, N, d)
+    for b in range(B):
+        for x in (c.k, c.v):
+            x.view(torch.uint8)[b, :, start[b]:] = 0x7f
+    k, v, q = queries(dt, B, T, H, d, 3), queries(dt, B, T, H, d, 4), queries(dt, B, T, Hq, d, 5)
+    st, n = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in (start, counts))
+    solar.history_cache_append(k, v, c, st, counts=n)
+    got = solar.history_cache_attention(q, c, st + T, 0.05, flags=solar.FLAG_CAUSAL)
+    for b in range(B - 1):
+        one = solar.HistoryCache(*(x[b:b + 1] for x in c))
+        near(got[b:b + 1, :counts[b]], q[b:b + 1, :counts[b]], one, [start[b] + counts[b]], 0.05, True, dt)
 
 
 def test_scores_of_any_size():
