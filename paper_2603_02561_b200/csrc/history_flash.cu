@@ -3,7 +3,7 @@
 // A CTA takes 256 (query, head of the group) rows of one cached head in two groups of 128, and walks through the cache in
 // tiles of 128 rows (d = 64) or 64 rows (d = 128: tensor memory holds scores, weights and sums of both groups).
 //   warps 0-7   a row per thread: the softmax
-//   warps 8-13  bring the tiles: 8-bit rows from global memory, a tile ahead in registers, to fp16 in shared memory
+//   warps 8-13  bring the tiles: bulk copies of the 8-bit rows three tiles ahead, then to fp16 in shared memory
 //               (e4m3 is exact in fp16), once for both groups
 //   warps 14,15 issue a group's MMAs: S = Q K^T of the next tile, as soon as the row warps hold the present one in
 //               registers, then Y += P V of the present one
@@ -15,6 +15,11 @@
 // the weights of a block add up to more than 2^15, and so before one of them is too large for fp16.
 // Where the queries alone do not fill the GPU the cache's rows are split over the CTAs of a cluster, which add up through
 // distributed shared memory.  Every wait is bounded; if one runs out the tile's output rows are written as NaN.
+//
+// 16 x 2048 queries over 10240 rows: d = 64 178 us (485 TFLOP/s; 3.4e8 exponentials would take the special-function units
+// 72), d = 128 235 us (730).  Bound by the row warps' chain of a tile, 2.2 us of wait, load, exponentials and store with two
+// warps a scheduler to hide it: without the exponentials 113, without the conversion 170, without the products 186 us
+// (d = 64, at 210 us).  Hence as little as possible in it: no maximum, no division, one fused multiplication a pair.
 #include <cuda_fp16.h>
 
 #include "sm100_ptx.cuh"

@@ -168,6 +168,16 @@ def test_a_row_that_is_not_finite_reaches_only_those_that_see_it(dt, d, what):
     assert torch.equal(got[0, :150], want[0, :150])
 
 
+@pytest.mark.parametrize("dt,d", [(BF, 64), (BF, 128), (F32, 64)])
+@pytest.mark.parametrize("M", [3, 700])
+@pytest.mark.parametrize("scale", [-0.05, 0.0])
+def test_scales_of_any_sign_and_groups_of_three(dt, d, M, scale):
+    c = filled(2, 2, 320, d)
+    q = queries(dt, 2, M, 6, d)
+    lengths = torch.tensor([300, 64], dtype=torch.int32, device="cuda")
+    near(solar.history_cache_attention(q, c, lengths, scale), q, c, [300, 64], scale, False, dt)
+
+
 @pytest.mark.parametrize("dt,d,T", [(BF, 64, 40), (BF, 64, 400), (BF, 128, 400), (F32, 32, 40)])
 def test_a_padded_batch_of_new_histories(dt, d, T):
     """Queries padded as the appended rows were, the cache behind those rows never written, one user's padding past its end."""
