@@ -607,18 +607,22 @@ linear_attention_kernel(const __grid_constant__ LinearParams prm) {
     *reinterpret_cast<uint4*>(op + (len + i / PIECES) * R.ot + (i % PIECES) * (16 / sizeof(T))) = make_uint4(0, 0, 0, 0);
 }
 
-constexpr int kMaxSegments = 8;      // CTAs of a cluster
+constexpr int kMaxSegments = 16;     // CTAs of a cluster
 
-// Segments per (user, head): the fewest waves x chunks of a CTA, where the pass over the keys and values that a
-// segmented history needs first costs about half of the pass that makes the outputs.
+// Segments per (user, head): the shortest estimate, waves x time of a CTA in tenths of a microsecond: 31 to start and end and 16 a
+// chunk; where the history is segmented 25 a chunk, the sums of its keys and values coming first, and 11 more for every CTA
+// of the cluster.  Sixteen CTAs only where all clusters find their SMs at once.  us a launch, 4 heads of 64 of one user: 200
+// events 9.6 whole, 10.2 in four; 1000 events 29, 25, 17.5, 16.4 in one, two, four, eight; 3000 events 26 in eight, 28 in
+// sixteen; 10240 events 99 in four, 46 in sixteen.
 template <typename F> int linear_segments(long long ctas, int T) {
   const int chunks = (T + F::C - 1) / F::C;
   const long long slots = (long long)kNumSMs * F::PER_SM;
   long long best = -1;
   int segs = 1;
-  for (int s = 1; s <= kMaxSegments && s <= chunks; ++s) {
+  for (int s = 1; s <= kMaxSegments && s <= chunks; s += s < 8 ? 1 : 8) {
+    if (s == 16 && ctas * s > kNumSMs) break;
     const long long waves = (ctas * s + slots - 1) / slots;
-    const long long per = (chunks + s - 1) / s, cost = waves * (s > 1 ? 3 * per + 4 : 2 * per);
+    const long long per = (chunks + s - 1) / s, cost = waves * (31 + (s > 1 ? 25 * per + 11 * s : 16 * per));
     if (best < 0 || cost < best) { best = cost; segs = s; }
   }
   return segs;
@@ -629,6 +633,14 @@ template <typename T, int D> cudaError_t launch_td(const LinearParams& prm, int 
   static bool limits_set[kMaxDevicesCached] = {};
   const cudaError_t e = set_kernel_limits(reinterpret_cast<const void*>(&linear_attention_kernel<T, D>), F::SMEM, limits_set);
   if (e != cudaSuccess) return e;
+  static bool wide[kMaxDevicesCached] = {};        // clusters of sixteen
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return cudaErrorInvalidDevice;
+  if (dev >= kMaxDevicesCached || !wide[dev]) {
+    const cudaError_t w = cudaFuncSetAttribute(reinterpret_cast<const void*>(&linear_attention_kernel<T, D>), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (w != cudaSuccess) return w;
+    if (dev < kMaxDevicesCached) wide[dev] = true;
+  }
   const int segs = linear_segments<F>((long long)B * prm.H * prm.roles, prm.T);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(segs, prm.H * prm.roles, B);

@@ -75,6 +75,11 @@ def test_segments_of_a_long_history(dt, d):
     check(dt, 2, 1100, 2, d, [1100, 259], True, scale=-0.1, strided=False)
 
 
+@pytest.mark.parametrize("dt,d", [(BF, 64), (BF, 128), (F32, 64)])
+def test_one_head_in_sixteen_segments(dt, d):
+    check(dt, 1, 7000, 1, d, [6999], True, scale=0.1)
+
+
 def test_states_left_out():
     check(BF, 1, 130, 3, 64, None, False)
     check(F32, 1, 130, 3, 64, [77], False)
