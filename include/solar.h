@@ -424,13 +424,16 @@ solar_status_t solar_linear_attention_step(int B, int H, int d, solar_dtype_t dt
  * The cache of B users, H heads and N rows a head (N a multiple of SOLAR_CACHE_BLOCK = 64):
  *   k8, v8            [B,H,N,d]    e4m3
  *   k_scale, v_scale  [B,H,N/64]   f32   one scale per block of 64 rows: a row is its bytes times the scale of its block
- * Scales are positive.  The append writes powers of two: the smallest 2^e, e >= -100, with max|x| <= 448 * 2^e over the block's rows.
+ * Scales are positive (below 2^-100 or above 2^120 sums over them may leave the range of fp32).  The append writes powers of
+ * two: the smallest 2^e, e >= -100, with max|x| <= 448 * 2^e over the block's rows.
  * Rows that were never written are never read as numbers; the cache needs no initial value.
  *
  * solar_history_cache_append: rows t = 0 .. counts[b] - 1 of K, V [B,T,H,d] dt become rows start[b] + t of user b,
  * rounded to the nearest e4m3 (what is not finite becomes NaN).  A block that held rows before start[b] keeps
- * them: where the new rows need a larger exponent, the older ones are rounded to it.  Rows at start[b] and behind it
- * are overwritten or left as they were.  Rows past N are dropped, and a start outside 0 .. N-1 writes nothing.
+ * them: its scale becomes the smallest power of two, 2^-100 to 2^120, that holds the new rows and is at or above the old scale
+ * (any positive number), and where that is another one the older rows are rounded to it.  Rows at start[b] and behind it are
+ * overwritten or left as they were; where a user has no new rows, nothing of it changes.  Rows past N are dropped, and a start
+ * outside 0 .. N-1 writes nothing.
  *   start  [B] int (in)       counts [B] int (in), taken as 0 .. T; NULL: T
  * The lengths are the caller's: lengths[b] = start[b] + counts[b] from then on.
  *

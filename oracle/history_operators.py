@@ -60,8 +60,17 @@ def scale_exponent(amax):
     return e
 
 
+def power_at_or_above(scale):
+    """Smallest e in -100 .. 120 with scale <= 2^e (120 where there is none: 448 * 2^120 is past what fp32 holds)."""
+    e = -100
+    while e < 120 and scale > 2.0 ** e:
+        e += 1
+    return e
+
+
 def append(cache, scales, rows, start, counts=None):
-    """In place: rows [B,T,H,d] into cache [B,H,N,d] (e4m3 values as floats) and scales [B,H,N/64]."""
+    """In place: rows [B,T,H,d] into cache [B,H,N,d] (e4m3 values as floats) and scales [B,H,N/64].  Older rows of a block are
+    rounded to its new scale from what they stand for."""
     B, T, H, d = rows.shape
     N = cache.shape[2]
     for b in range(B):
@@ -79,9 +88,9 @@ def append(cache, scales, rows, start, counts=None):
                 x = np.where(np.isfinite(x), x, np.nan)
                 e = scale_exponent(np.nanmax(np.abs(x), initial=0.0))
                 if lo > blk * BLOCK:
-                    old = int(np.log2(scales[b, h, blk]))
-                    e = max(e, old)
-                    cache[b, h, blk * BLOCK:lo] = round_e4m3(cache[b, h, blk * BLOCK:lo] * 2.0 ** (old - e))
+                    old = float(scales[b, h, blk])
+                    e = max(e, power_at_or_above(old))
+                    cache[b, h, blk * BLOCK:lo] = np.clip(round_e4m3(cache[b, h, blk * BLOCK:lo] * (old * 2.0 ** -e)), -448.0, 448.0)
                 scales[b, h, blk] = 2.0 ** e
                 cache[b, h, lo:hi] = round_e4m3(x * 2.0 ** -e)
 

@@ -5,7 +5,8 @@
 // at every magnitude down to 2^-6, so a scale between two powers of two would gain nothing; and with whole powers a scale
 // comes out of a sum as an exact factor, and a block whose exponent grows when a later row comes in is moved to the
 // new exponent without another rounding (but for values under 2^-14 of the block's largest, which e4m3 holds as
-// fractions of 2^-9).
+// fractions of 2^-9).  A block that another program filled may have any positive scale; the append rounds its rows to a
+// power of two, from what they stand for.
 //
 // history_append_kernel: a CTA per block of the cache that the new rows touch, head and K or V.
 //
@@ -36,9 +37,14 @@ namespace solar {
 namespace {
 
 constexpr int kBlock = SOLAR_CACHE_BLOCK;          // rows that share a scale
-constexpr int kMinExp = -100, kMaxExp = 120;       // of a scale: 448 * 2^120 is the last value below 2^129
+constexpr int kMinExp = -100, kMaxExp = 120;       // of a scale that the append writes: 448 * 2^120 is past what fp32 holds
 
 __device__ __forceinline__ float two_to(int e) { return __int_as_float((e + 127) << 23); }   // -126 <= e <= 127
+// a * f without a second rounding to come: cut off, and its last bit set where something was (24 bits before the four of e4m3)
+__device__ __forceinline__ float mul_odd(float a, float f) {
+  const float p = __fmul_rz(a, f);
+  return fmaf(a, f, -p) == 0.f ? p : __uint_as_float(__float_as_uint(p) | 1u);
+}
 __device__ __forceinline__ int exponent_of(float x) { return (int)((__float_as_uint(x) >> 23) & 0xffu) - 127; }
 // Two floats to e4m3, nearest even; what is not finite becomes NaN.
 __device__ __forceinline__ uint32_t to_e4m3x2(float a, float b) {
@@ -84,6 +90,7 @@ history_append_kernel(LinearOperand k, LinearOperand v, int T_new, int N, const 
   uint8_t* cache = (value ? v8 : k8) + (((size_t)b * H + h) * N + (size_t)blk * kBlock) * D;
   float* scale = (value ? v_scale : k_scale) + ((size_t)b * H + h) * (N / kBlock) + blk;
   const int lo = max(first - blk * kBlock, 0), hi = min(end - blk * kBlock, kBlock);      // the new rows of this block
+  if (lo >= hi) return;                                           // (no new row: nothing of the block changes)
   const float before = lo > 0 ? ld_dep(scale) : 0.f;
 
   float x[CH][16], m = 0.f;
@@ -107,9 +114,11 @@ history_append_kernel(LinearOperand k, LinearOperand v, int T_new, int N, const 
   // 448 = 1.75 * 2^8
   int e = exponent_of(m) - 8 + ((__float_as_uint(m) & 0x7fffffu) > 0x600000u ? 1 : 0);
   e = max(e, kMinExp);
-  const int e_old = lo > 0 ? min(max(exponent_of(before), kMinExp), kMaxExp) : e;
-  e = max(e, e_old);
-  const float inv = two_to(-e);
+  if (lo > 0) {                                                   // at least the smallest power at or above the old scale
+    const int old = exponent_of(before) + ((__float_as_uint(before) & 0x7fffffu) != 0 ? 1 : 0);
+    e = max(e, min(max(old, kMinExp), kMaxExp));
+  }
+  const float inv = two_to(-e), moved = lo > 0 ? before * inv : 1.f;        // what the older rows' bytes are multiplied by
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
     const int i = tid + c * NT, row = i / PIECES, piece = i % PIECES;
@@ -120,20 +129,19 @@ history_append_kernel(LinearOperand k, LinearOperand v, int T_new, int N, const 
       for (int q = 0; q < 4; ++q)
         w[q] = to_e4m3x2(x[c][4 * q] * inv, x[c][4 * q + 1] * inv) | (to_e4m3x2(x[c][4 * q + 2] * inv, x[c][4 * q + 3] * inv) << 16);
       *at = make_uint4(w[0], w[1], w[2], w[3]);
-    } else if (row < lo && e > e_old) {                           // older rows of the block, to the new exponent
-      const float f = two_to(max(e_old - e, -126));
+    } else if (row < lo && moved != 1.f) {                        // older rows of the block, to the new scale
       const uint4 o = ld_dep(at);
       const uint32_t u[4] = {o.x, o.y, o.z, o.w};
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const uint32_t a = e4m3x2_to_half2(u[q] & 0xffffu), d = e4m3x2_to_half2(u[q] >> 16);
         const float2 fa = __half22float2(*reinterpret_cast<const __half2*>(&a)), fd = __half22float2(*reinterpret_cast<const __half2*>(&d));
-        w[q] = to_e4m3x2(fa.x * f, fa.y * f) | (to_e4m3x2(fd.x * f, fd.y * f) << 16);
+        w[q] = to_e4m3x2(mul_odd(fa.x, moved), mul_odd(fa.y, moved)) | (to_e4m3x2(mul_odd(fd.x, moved), mul_odd(fd.y, moved)) << 16);
       }
       *at = make_uint4(w[0], w[1], w[2], w[3]);
     }
   }
-  if (tid == 0 && (lo == 0 || e > e_old)) *scale = two_to(e);
+  if (tid == 0) *scale = two_to(e);
 }
 
 // ---- attention ----------------------------------------------------------------------------------------
