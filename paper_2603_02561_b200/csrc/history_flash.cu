@@ -13,6 +13,9 @@
 // where m is the largest z so far: P is then exact to fp16's 11 bits wherever the product of weight and value scale is
 // within 2^-17 of the row's largest (and to 2^-28 of that largest below), which is what the output is rounded by.  m is raised (Y and l rescaled) only when
 // the weights of a block add up to more than 2^15, and so before one of them is too large for fp16.
+// The weights of a block whose value scale lies 2^64 or more below the largest one so far (one of zeros, whose scale is 2^-100,
+// beside values of any size) may vanish from 2^(z - m) although they count in l: such a block is added to l by exponentials
+// of its own, relative to its own maximum, and l is rescaled in two steps where m rises by more than fp32 has exponents.
 // Where the queries alone do not fill the GPU the cache's rows are split over the CTAs of a cluster, which add up through
 // distributed shared memory.  Every wait is bounded; if one runs out the tile's output rows are written as NaN.
 //
@@ -34,6 +37,7 @@ constexpr int kConvWarp = 8, kConvWarps = 6, kMmaWarp = 14, kThreads = 512, kCon
 constexpr int kRowRegs = 192, kOtherRegs = 64;     // 256 threads each: together what the block is launched with, 512 x 128
 constexpr int kStages = 3, kMaxSplits = 8;
 constexpr float kLift = 3.f;
+constexpr float kFar = 64.f;                       // a weight lost to fp32's range is then under 2^-65 of l
 constexpr int kErrKv = 0x41, kErrFree = 0x42, kErrS = 0x43, kErrSf = 0x44, kErrP = 0x45, kErrY = 0x46, kErrRaw = 0x47;
 
 template <int D> struct HfCfg {
@@ -88,7 +92,7 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
   uint8_t* sKV = base + F::Q_BYTES;                // [stages][K, V][KB][NTOK][128 B]
   uint8_t* sRaw = sKV + kStages * F::STAGE;        // [stages][K, V][NTOK][D B]
   __shared__ __align__(8) uint64_t raw_full[kStages], kv_full[kStages], kv_free[kStages], s_full[kGroups], s_free[kGroups], p_full[kGroups], y_done[kGroups], bar_end;
-  __shared__ float4 s_scale[kStages][NB];          // ks, log2 vs, 2^-3 / vs of a block
+  __shared__ float4 s_scale[kStages][NB];          // ks, log2 vs, 2^-3 / vs (0 where far), whether far below the largest vs, of a block
   __shared__ int s_odd[kStages];                   // a value that some of the tile's queries do not see is not finite
   __shared__ uint32_t s_tmem;
   __shared__ int s_err;
@@ -183,12 +187,13 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
       bulk_load(sRaw + (t % kStages) * F::RAW, kc + (size_t)first * D, bytes, &raw_full[t % kStages]);
       bulk_load(sRaw + (t % kStages) * F::RAW + F::RAW / 2, vc + (size_t)first * D, bytes, &raw_full[t % kStages]);
     };
-    float ks = 1.f, vs = 1.f;                      // scale of block ct of the tile
+    float ks = 1.f, vs = 0.f;                      // scale of block ct of the tile
+    float lv_top = -INFINITY;                      // log2 of the largest value scale so far
     auto scales = [&](int t) {
       const int blk = (t0 + t) * NB + ct;
       const bool held = ct < NB && blk * kBlock < len;
       ks = held ? ld_dep(ksc + blk) : 1.f;
-      vs = held ? ld_dep(vsc + blk) : 1.f;
+      vs = held ? ld_dep(vsc + blk) : 0.f;
     };
     int issued = 0;
     if (ct == 0)
@@ -223,9 +228,11 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
         *reinterpret_cast<uint4*>(box + ptx::swz128(r, 2 * (p % 4) + 1)) = make_uint4(f.x, f.y, g.x, g.y);
       }
       if (ct == 0) s_odd[st] = 0;
-      if (ct < NB) {
+      if (warp == kConvWarp) {
         const float lv = vs < 1.1754944e-38f ? -126.f : log2f(vs);
-        s_scale[st][ct] = make_float4(ks, lv, exp2f(-lv - kLift), 0.f);
+        lv_top = fmaxf(lv_top, NB == 2 ? fmaxf(lv, __shfl_xor_sync(0xffffffffu, lv, 1)) : lv);
+        const bool far = lv < lv_top - kFar;
+        if (ct < NB) s_scale[st][ct] = make_float4(ks, lv, far ? 0.f : exp2f(-lv - kLift), far ? 1.f : 0.f);
       }
       asm volatile("bar.sync 1, %0;" ::"n"(kConvThreads) : "memory");
       if (ct == 0 && issued < nt && *err == 0) copy(issued++);  // everybody has read the tile's bytes
@@ -331,8 +338,9 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
             m_tile = fmaxf(m_tile, fmaf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), f[n], sc[n].y));
           }
           const float m_new = fmaxf(m_ref, m_tile), alpha = m_ref == -INFINITY ? 0.f : ptx::fast_exp2(m_ref - m_new);
+          const float root = m_ref == -INFINITY ? 0.f : ptx::fast_exp2(0.5f * (m_ref - m_new));
           m_ref = m_new;
-          l_run *= alpha;
+          l_run = l_run * root * root;             // (l is up to 2^100 and more where value scales are small)
           if (t > 0) {
 #pragma unroll
             for (int c0 = 0; c0 < D; c0 += 16) {
@@ -382,6 +390,17 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
         if (!look) break;
       }
       l_run += add;
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        if (*(volatile float*)&s_scale[st][n].w == 0.f) continue;
+        float top = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < kBlock; ++j) top = fmaxf(top, fmaf(s[n * kBlock + j], f[n], off[n]));
+        if (top == -INFINITY) continue;
+#pragma unroll
+        for (int j = 0; j < kBlock; ++j) sum += ptx::fast_exp2(fmaf(s[n * kBlock + j], f[n], off[n]) - top);
+        l_run = fmaf(sum, exp2f(top - kLift - *(volatile float*)&s_scale[st][n].y), l_run);
+      }
       if (odd) {                                   // a value that is not finite, for the queries that see it
         for (int j = first; j < min(limit, first + NTOK); ++j)
           for (int i = 0; i < D; ++i)
@@ -449,7 +468,8 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
       for (int w = 0; w < kMaxSplits; ++w) {
         if (w >= splits) break;
         const float f = ms[w] == -INFINITY ? 0.f : exp2f(ms[w] - top);
-        l = fmaf(f, ls[w], l);
+        const float root = ms[w] == -INFINITY ? 0.f : exp2f(0.5f * (ms[w] - top));
+        l = fmaf(ls[w] * root, root, l);
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
           const float4 y = ptx::ld_cluster_f4(reinterpret_cast<const float4*>(base) + (2 * piece + q) * kRows + r, w);

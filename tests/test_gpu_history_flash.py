@@ -248,3 +248,50 @@ def test_queries_may_be_overwritten():
         want = attend(q, c, [2112, 1500, 0], 0.1, False, kernel)
         solar.history_cache_attention(q, c, n, 0.1, O=q)
         assert torch.equal(q, want)
+
+
+# ---- values of very different size ----------------------------------------------------------------------
+def spread_values(c, exponents, rise):
+    """Value blocks of 2^e in turn, zeros where e is the smallest of all; `rise`: how much larger (in log2 units) the scores of the zero
+    blocks are, by component 0 of the keys."""
+    B, H, N, d = c.k.shape
+    at = torch.arange(N // 64) % len(exponents)
+    e = torch.tensor(exponents)[at]
+    zero = (e == min(exponents)).cuda()
+    c.v_scale.copy_(torch.exp2(e.double()).float().expand(B, H, N // 64))
+    c.v.view(torch.uint8).view(B, H, N // 64, 64, d)[:, :, zero] = 0
+    c.k_scale.fill_(2.0 ** -6)
+    one = int(torch.tensor([64.0 if rise > 0 else -64.0]).to(E4).view(torch.uint8))
+    k = c.k.view(torch.uint8).view(B, H, N // 64, 64, d)
+    k[..., 0] = 0
+    if rise:
+        k[:, :, zero, :, 0] = one
+
+
+@pytest.mark.parametrize("kernel", [FLASH, FEW])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("exponents", [[-100, 31], [31, -100, 0], [-100, 60, 0], [60, -100], [0, -100], [20, 5, -100], [0, 0, 0, 0, 0, 0, -100, 31, 31]])
+@pytest.mark.parametrize("rise", [0, 20, 130, -20])
+def test_value_scales_far_apart(kernel, d, exponents, rise):
+    """Blocks of zeros (their scale is 2^-100) beside blocks of large values count in the softmax as any others do."""
+    B, M, Hq, H, N = SIZES[kernel]
+    c, q = filled(B, H, N, d), queries(B, M, Hq, d)
+    spread_values(c, exponents, rise)
+    q[..., 0] = 1.0
+    scale = abs(rise) * np.log(2.0) if rise else 0.05        # component 0 of the zero blocks' keys is 1 (or -1)
+    if rise:
+        q[..., 1:] *= 2.0 ** -6
+    lengths = [2112, 1500, 70]
+    near(attend(q, c, lengths, scale, False, kernel), q, c, lengths, scale, False, [0, 1, M - 1], kernel)
+
+
+@pytest.mark.parametrize("kernel", [FLASH])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("e", [90, 105])
+def test_largest_values(kernel, d, e):
+    """Values of up to 448 * 2^105, and zeros: the weighted mean is far inside of what bf16 holds."""
+    B, M, Hq, H, N = SIZES[kernel]
+    c, q = filled(B, H, N, d), queries(B, M, Hq, d)
+    spread_values(c, [e, -100, 0], 0)
+    lengths = [2112, 1500, 70]
+    near(attend(q, c, lengths, 0.05, False, kernel), q, c, lengths, 0.05, False, [0, 1, M - 1], kernel)
