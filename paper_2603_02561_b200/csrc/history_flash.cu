@@ -92,8 +92,8 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
   uint8_t* sKV = base + F::Q_BYTES;                // [stages][K, V][KB][NTOK][128 B]
   uint8_t* sRaw = sKV + kStages * F::STAGE;        // [stages][K, V][NTOK][D B]
   __shared__ __align__(8) uint64_t raw_full[kStages], kv_full[kStages], kv_free[kStages], s_full[kGroups], s_free[kGroups], p_full[kGroups], y_done[kGroups], bar_end;
-  __shared__ float4 s_scale[kStages][NB];          // ks, log2 vs, 2^-3 / vs (0 where far), whether far below the largest vs, of a block
-  __shared__ int s_odd[kStages];                   // a value that some of the tile's queries do not see is not finite
+  __shared__ float4 s_scale[kStages][NB];          // ks, log2 vs, 2^-3 / vs (0 where far below the largest vs) of a block
+  __shared__ int s_odd[kStages];                   // bit 0: a value that some of the tile's queries do not see is not finite; then a bit a block: far
   __shared__ uint32_t s_tmem;
   __shared__ int s_err;
 
@@ -227,17 +227,18 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
         *reinterpret_cast<uint4*>(box + ptx::swz128(r, 2 * (p % 4))) = make_uint4(a.x, a.y, d.x, d.y);
         *reinterpret_cast<uint4*>(box + ptx::swz128(r, 2 * (p % 4) + 1)) = make_uint4(f.x, f.y, g.x, g.y);
       }
-      if (ct == 0) s_odd[st] = 0;
       if (warp == kConvWarp) {
         const float lv = vs < 1.1754944e-38f ? -126.f : log2f(vs);
         lv_top = fmaxf(lv_top, NB == 2 ? fmaxf(lv, __shfl_xor_sync(0xffffffffu, lv, 1)) : lv);
         const bool far = lv < lv_top - kFar;
-        if (ct < NB) s_scale[st][ct] = make_float4(ks, lv, far ? 0.f : exp2f(-lv - kLift), far ? 1.f : 0.f);
+        if (ct < NB) s_scale[st][ct] = make_float4(ks, lv, far ? 0.f : exp2f(-lv - kLift), 0.f);
+        const uint32_t which = __ballot_sync(0xffffffffu, far) & ((1u << NB) - 1);
+        if (ct == 0) s_odd[st] = (int)(which << 1);
       }
       asm volatile("bar.sync 1, %0;" ::"n"(kConvThreads) : "memory");
       if (ct == 0 && issued < nt && *err == 0) copy(issued++);  // everybody has read the tile's bytes
       if (t + 1 < nt) scales(t + 1);
-      if (odd) s_odd[st] = 1;
+      if (odd) atomicOr(&s_odd[st], 1);
       ptx::fence_proxy_async_smem();
       ptx::mbar_arrive_warp(&kv_full[st], lane);
     }
@@ -390,21 +391,22 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
         if (!look) break;
       }
       l_run += add;
+      if (odd != 0) {
 #pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        if (*(volatile float*)&s_scale[st][n].w == 0.f) continue;
-        float top = -INFINITY, sum = 0.f;
+        for (int n = 0; n < NB; ++n) {             // blocks whose value scale is far below the largest
+          if ((odd >> (n + 1) & 1) == 0) continue;
+          float top = -INFINITY, sum = 0.f;
 #pragma unroll
-        for (int j = 0; j < kBlock; ++j) top = fmaxf(top, fmaf(s[n * kBlock + j], f[n], off[n]));
-        if (top == -INFINITY) continue;
+          for (int j = 0; j < kBlock; ++j) top = fmaxf(top, fmaf(s[n * kBlock + j], f[n], off[n]));
+          if (top == -INFINITY) continue;
 #pragma unroll
-        for (int j = 0; j < kBlock; ++j) sum += ptx::fast_exp2(fmaf(s[n * kBlock + j], f[n], off[n]) - top);
-        l_run = fmaf(sum, exp2f(top - kLift - *(volatile float*)&s_scale[st][n].y), l_run);
-      }
-      if (odd) {                                   // a value that is not finite, for the queries that see it
-        for (int j = first; j < min(limit, first + NTOK); ++j)
-          for (int i = 0; i < D; ++i)
-            if ((vc[(size_t)j * D + i] & 0x7f) == 0x7f) l_run = __int_as_float(0x7fffffff);
+          for (int j = 0; j < kBlock; ++j) sum += ptx::fast_exp2(fmaf(s[n * kBlock + j], f[n], off[n]) - top);
+          l_run = fmaf(sum, exp2f(top - kLift - *(volatile float*)&s_scale[st][n].y), l_run);
+        }
+        if (odd & 1)                               // a value that is not finite, for the queries that see it
+          for (int j = first; j < min(limit, first + NTOK); ++j)
+            for (int i = 0; i < D; ++i)
+              if ((vc[(size_t)j * D + i] & 0x7f) == 0x7f) l_run = __int_as_float(0x7fffffff);
       }
       ptx::tmem_st_wait();
       ptx::tc_fence_before_sync();
