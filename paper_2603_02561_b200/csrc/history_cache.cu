@@ -391,6 +391,8 @@ history_attention_kernel(LinearOperand q, T* O, long long ob, long long ot, long
 #pragma unroll
       for (int t = 0; t < NP; ++t) { pa[t][n >> 1][2 * (n & 1)] = a[t]; pa[t][n >> 1][2 * (n & 1) + 1] = c[t]; }
     }
+    // a block that some of the tile's queries do not see may hold nothing yet, and its scale be anything
+    if (!whole && !(fabsf(vs) < INFINITY)) vs = 0.f;
     rows_wait<1>();                                // this block's values
     __syncwarp();
     bool odd = false;                              // a value of the block that is not finite

@@ -228,9 +228,13 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
         *reinterpret_cast<uint4*>(box + ptx::swz128(r, 2 * (p % 4) + 1)) = make_uint4(f.x, f.y, g.x, g.y);
       }
       if (warp == kConvWarp) {
+        // a block that some queries do not see may hold nothing yet, and its scale be anything
+        const bool part = c.causal && first + (ct + 1) * kBlock > least;
+        if (part && !(fabsf(ks) < INFINITY)) ks = 1.f;
+        if (part && !(fabsf(vs) < INFINITY)) vs = 0.f;
         const float lv = vs < 1.1754944e-38f ? -126.f : log2f(vs);
         lv_top = fmaxf(lv_top, NB == 2 ? fmaxf(lv, __shfl_xor_sync(0xffffffffu, lv, 1)) : lv);
-        const bool far = lv < lv_top - kFar;
+        const bool far = lv < lv_top - kFar && !(part && vs == 0.f);
         if (ct < NB) s_scale[st][ct] = make_float4(ks, lv, far ? 0.f : exp2f(-lv - kLift), 0.f);
         const uint32_t which = __ballot_sync(0xffffffffu, far) & ((1u << NB) - 1);
         if (ct == 0) s_odd[st] = (int)(which << 1);

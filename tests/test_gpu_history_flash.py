@@ -295,3 +295,31 @@ def test_largest_values(kernel, d, e):
     spread_values(c, [e, -100, 0], 0)
     lengths = [2112, 1500, 70]
     near(attend(q, c, lengths, 0.05, False, kernel), q, c, lengths, 0.05, False, [0, 1, M - 1], kernel)
+
+
+# ---- a cache whose memory was never set -----------------------------------------------------------------
+@pytest.mark.parametrize("kernel", [FLASH, FEW])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("left", [float("nan"), float("inf"), -float("inf"), 3e38, 0.0])
+def test_scales_that_were_never_written_are_not_read_as_numbers(kernel, d, left):
+    """A padded batch in a cache of arbitrary memory: the padding's queries see blocks that hold nothing yet, in tiles that a
+    user's own queries share."""
+    B, H, Hq, N = 3, 2, 4, 2112
+    T = 1200 if kernel == FLASH else 13
+    start, counts = [60, 125, 0], [2, 7, 0]
+    c = filled(B, H, N, d)
+    clean = solar.HistoryCache(*(x.clone() for x in c))
+    for b in range(B):
+        at = -(-(start[b] + counts[b]) // 64)
+        for x, s in ((c.k, c.k_scale), (c.v, c.v_scale)):
+            s[b, :, at:] = left
+            x.view(torch.uint8)[b, :, start[b]:] = 0x7f
+    k, v, q = queries(B, T, H, d, 3), queries(B, T, H, d, 4), queries(B, T, Hq, d, 5)
+    st, n = (torch.tensor(x, dtype=I32, device="cuda") for x in (start, counts))
+    solar.history_cache_append(k, v, clean, st, counts=n)
+    solar.history_cache_append(k, v, c, st, counts=n)
+    out = attend(q, c, [y + T for y in start], 0.05, True, kernel)
+    for b in (0, 1):
+        one, m = solar.HistoryCache(*(x[b:b + 1] for x in clean)), counts[b]
+        assert torch.isfinite(out[b:b + 1, :m]).all()
+        near(out[b:b + 1, :m], q[b:b + 1, :m], one, [start[b] + m], 0.05, True, range(m), kernel)
