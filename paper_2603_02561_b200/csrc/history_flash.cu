@@ -23,6 +23,8 @@
 // 72), d = 128 235 us (730).  Bound by the row warps' chain of a tile, 2.2 us of wait, load, exponentials and store with two
 // warps a scheduler to hide it: without the exponentials 113, without the conversion 170, without the products 186 us
 // (d = 64, at 210 us).  Hence as little as possible in it: no maximum, no division, one fused multiplication a pair.
+#include <climits>
+
 #include <cuda_fp16.h>
 
 #include "sm100_ptx.cuh"
@@ -120,7 +122,7 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
     if (!c.causal) return len;
     return (int)max(min((long long)len, (long long)told - c.M + row / c.G + 1), 0ll);
   };
-  const int reach = limit_of(min(row0 + kRows, rows) - 1), least = limit_of(row0);
+  const int reach = limit_of(min(row0 + kRows, rows) - 1), least = c.causal ? limit_of(row0) : INT_MAX;      // rows that every query sees
   const int all = (reach + NTOK - 1) / NTOK, per = (all + splits - 1) / splits;
   const int t0 = min(split * per, all), nt = min(per, all - t0);
   const uint8_t* kc = c.k8 + ((size_t)b * c.H + hk) * c.N * D;
@@ -205,7 +207,7 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
       ptx::mbar_wait(&raw_full[st], (t / kStages) & 1, err, kErrRaw);
       if (t >= kStages) ptx::mbar_wait(&kv_free[st], (t / kStages - 1) & 1, err, kErrFree);
       __syncwarp();
-      const bool mixed = first + NTOK > least && c.causal;      // some queries do not see all of the tile's rows
+      const bool mixed = first + NTOK > least;      // some queries do not see all of the tile's rows
       bool odd = false;
 #pragma unroll
       for (int i = 0; i < F::PER; ++i) {
@@ -229,12 +231,11 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
       }
       if (warp == kConvWarp) {
         // a block that some queries do not see may hold nothing yet, and its scale be anything
-        const bool part = c.causal && first + (ct + 1) * kBlock > least;
-        if (part && !(fabsf(ks) < INFINITY)) ks = 1.f;
-        if (part && !(fabsf(vs) < INFINITY)) vs = 0.f;
+        if (mixed && !(fabsf(ks) < INFINITY)) ks = 1.f;
+        if (mixed && !(fabsf(vs) < INFINITY)) vs = 0.f;
         const float lv = vs < 1.1754944e-38f ? -126.f : log2f(vs);
         lv_top = fmaxf(lv_top, NB == 2 ? fmaxf(lv, __shfl_xor_sync(0xffffffffu, lv, 1)) : lv);
-        const bool far = lv < lv_top - kFar && !(part && vs == 0.f);
+        const bool far = lv < lv_top - kFar && !(mixed && vs == 0.f);
         if (ct < NB) s_scale[st][ct] = make_float4(ks, lv, far ? 0.f : exp2f(-lv - kLift), 0.f);
         const uint32_t which = __ballot_sync(0xffffffffu, far) & ((1u << NB) - 1);
         if (ct == 0) s_odd[st] = (int)(which << 1);
