@@ -176,6 +176,7 @@ constexpr int kRowsPerCta = 16, kWarps = 4, kMaxSplits = 16;
 // CTAs that an SM is to hold, by registers
 template <typename T, int D> constexpr int kPerSm = D == 128 ? 2 : D == 64 || sizeof(T) == 4 ? 3 : 4;
 constexpr float kLift = 15.f;                      // log2 of the largest weight as fp16 holds it
+constexpr float kUnlift = 0x1p-15f;
 
 template <int D> struct HistShared {
   // A warp's rows on their way: keys of two blocks, values of one.
@@ -393,6 +394,7 @@ history_attention_kernel(LinearOperand q, T* O, long long ob, long long ot, long
     }
     // a block that some of the tile's queries do not see may hold nothing yet, and its scale be anything
     if (!whole && !(fabsf(vs) < INFINITY)) vs = 0.f;
+    vs *= kUnlift;                                 // the weights' lift ends here: sums over large values need the exponents
     rows_wait<1>();                                // this block's values
     __syncwarp();
     bool odd = false;                              // a value of the block that is not finite
@@ -553,7 +555,7 @@ history_attention_kernel(LinearOperand q, T* O, long long ob, long long ot, long
       const long long mq = out / G;
       T* p = O + (long long)b * ob + mq * ot + (long long)(hk * G + (int)(out - mq * G)) * oh + piece * 4;
       // l = 0: a query that sees no row at all (a NaN in l or m is none: it goes on to the output)
-      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const float inv = l == 0.f ? 0.f : 0x1p15f / l;            // (l has the lift, the sums have not)
       if constexpr (sizeof(T) == 2)
         *reinterpret_cast<uint2*>(p) = make_uint2(ptx::pack_bf16(a.x * inv, a.y * inv), ptx::pack_bf16(a.z * inv, a.w * inv));
       else

@@ -285,7 +285,7 @@ def test_value_scales_far_apart(kernel, d, exponents, rise):
     near(attend(q, c, lengths, scale, False, kernel), q, c, lengths, scale, False, [0, 1, M - 1], kernel)
 
 
-@pytest.mark.parametrize("kernel", [FLASH])
+@pytest.mark.parametrize("kernel", [FLASH, FEW])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("e", [90, 105])
 def test_largest_values(kernel, d, e):
