@@ -238,9 +238,9 @@ linear_attention_kernel(const __grid_constant__ LinearParams prm) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) st[n][i] = 0.f;
   // bf16 storage: three terms of a decayed key, and sums outside of the state's accumulators (of the chunk, d = 128: of
-  // 16 events, by registers), go in where they count, in the state that is returned.  A chunk whose last event has
-  // decayed to less than 2^-3 by then gets two terms straight into the accumulators (2.4e-6 of the sum, an eighth of
-  // that in the state), as all do where no state is returned.
+  // 16 events, by registers), go in where they count, in the state that is returned.  A chunk with events behind it, whose
+  // own last event they let decay to less than 2^-3, gets two terms straight into the accumulators (2.4e-6 of its sum, which
+  // is an eighth of that in a state of events of one size), as all do where no state is returned.
   auto update_as = [&](uint32_t sk, uint32_t sv, int n_real, auto kind) {
     constexpr int TERMS = decltype(kind)::value;
     constexpr bool NEAR = NP == 1 && TERMS == 3 && D < 128, EXACT = NP == 3 || (TERMS == 3 && D == 128);
@@ -308,7 +308,8 @@ linear_attention_kernel(const __grid_constant__ LinearParams prm) {
   auto update = [&](uint32_t sk, uint32_t sv, int c) {
     const int n_real = min(C, len - c * C);
     if constexpr (NP == 1) {
-      if (R.s1 == nullptr || (float)max(len - (c + 1) * C, 1) * l2 < -3.f) {
+      const int after = len - (c + 1) * C;         // events behind the chunk; the last one is the state as it is returned
+      if (R.s1 == nullptr || (after > 0 && (float)after * l2 < -3.f)) {
         update_as(sk, sv, n_real, std::integral_constant<int, 2>{});
         return;
       }
