@@ -37,7 +37,9 @@ constexpr int kBlock = SOLAR_CACHE_BLOCK;
 constexpr int kGroupRows = 128, kGroups = 2, kRows = kGroupRows * kGroups;
 constexpr int kConvWarp = 8, kConvWarps = 6, kMmaWarp = 14, kThreads = 512, kConvThreads = kConvWarps * 32;
 constexpr int kRowRegs = 192, kOtherRegs = 64;     // 256 threads each: together what the block is launched with, 512 x 128
+constexpr int kScaleWarp = kConvWarp + kConvWarps - 1;
 constexpr int kStages = 3, kMaxSplits = 8;
+constexpr int kBatch = 32;                         // blocks whose scales are looked at together, one a lane
 constexpr float kLift = 3.f;
 constexpr float kFar = 64.f;                       // a weight lost to fp32's range is then under 2^-65 of l
 constexpr int kErrKv = 0x41, kErrFree = 0x42, kErrS = 0x43, kErrSf = 0x44, kErrP = 0x45, kErrY = 0x46, kErrRaw = 0x47;
@@ -94,8 +96,10 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
   uint8_t* sKV = base + F::Q_BYTES;                // [stages][K, V][KB][NTOK][128 B]
   uint8_t* sRaw = sKV + kStages * F::STAGE;        // [stages][K, V][NTOK][D B]
   __shared__ __align__(8) uint64_t raw_full[kStages], kv_full[kStages], kv_free[kStages], s_full[kGroups], s_free[kGroups], p_full[kGroups], y_done[kGroups], bar_end;
-  __shared__ float4 s_scale[kStages][NB];          // ks, log2 vs, 2^-3 / vs (0 where far below the largest vs) of a block
-  __shared__ int s_odd[kStages];                   // bit 0: a value that some of the tile's queries do not see is not finite; then a bit a block: far
+  // Of the blocks of this CTA's range, the last 64 looked at: ks, log2 vs, 2^-3 / vs (0 where far), 2 where vs is far below the largest
+  __shared__ float4 s_scale[2 * kBatch];
+  __shared__ float s_next[2][kBatch];              // ks and vs of the next 32 blocks, on their way
+  __shared__ int s_odd[kStages];                   // a value that some of the tile's queries do not see is not finite
   __shared__ uint32_t s_tmem;
   __shared__ int s_err;
 
@@ -189,24 +193,50 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
       bulk_load(sRaw + (t % kStages) * F::RAW, kc + (size_t)first * D, bytes, &raw_full[t % kStages]);
       bulk_load(sRaw + (t % kStages) * F::RAW + F::RAW / 2, vc + (size_t)first * D, bytes, &raw_full[t % kStages]);
     };
-    float ks = 1.f, vs = 0.f;                      // scale of block ct of the tile
+    // Scales are brought and looked at by the first of these warps, 32 blocks at a time (one tile's at a time, in the path of its
+    // conversion: d = 128 250 us in the place of 229).
     float lv_top = -INFINITY;                      // log2 of the largest value scale so far
-    auto scales = [&](int t) {
-      const int blk = (t0 + t) * NB + ct;
-      const bool held = ct < NB && blk * kBlock < len;
-      ks = held ? ld_dep(ksc + blk) : 1.f;
-      vs = held ? ld_dep(vsc + blk) : 0.f;
+    auto fetch_scales = [&](int from) {            // blocks of this CTA's range from .. from + 31
+      const int blk = t0 * NB + from + lane;
+      const bool held = from < nt * NB && blk * kBlock < len;
+      const uint32_t n = held ? 4 : 0;             // (zeros in the place of those that are not read)
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(ptx::smem_u32(&s_next[0][lane])), "l"(ksc + (held ? blk : 0)), "r"(n) : "memory");
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(ptx::smem_u32(&s_next[1][lane])), "l"(vsc + (held ? blk : 0)), "r"(n) : "memory");
+    };
+    auto take_scales = [&](int from) {
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      float ks = s_next[0][lane], vs = s_next[1][lane];         // (a lane reads what it has brought itself)
+      // a block that some queries do not see may hold nothing yet, and its scale be anything
+      const bool part = (t0 * NB + from + lane + 1) * kBlock > least;
+      if (part && !(fabsf(ks) < INFINITY)) ks = 1.f;
+      if (part && !(fabsf(vs) < INFINITY)) vs = 0.f;
+      const float lv = vs < 1.1754944e-38f ? -126.f : log2f(vs);
+      // the largest scale up to this block's tile, the tile's other block included
+      float top = fmaxf(lv_top, NB == 2 ? fmaxf(lv, __shfl_xor_sync(0xffffffffu, lv, 1)) : lv);
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const float other = __shfl_up_sync(0xffffffffu, top, d);
+        if (lane >= d) top = fmaxf(top, other);
+      }
+      lv_top = __shfl_sync(0xffffffffu, top, 31);
+      const bool far = lv < top - kFar && !(part && vs == 0.f);
+      s_scale[(from & kBatch) + lane] = make_float4(ks, lv, far ? 0.f : exp2f(-lv - kLift), __int_as_float(far ? 2 : 0));
     };
     int issued = 0;
     if (ct == 0)
       for (; issued < min(nt, kStages); ++issued) copy(issued);
-    if (nt > 0) scales(0);
+    if (warp == kScaleWarp) fetch_scales(0);
     for (int t = 0; t < nt; ++t) {
       const int st = t % kStages, first = (t0 + t) * NTOK;
       const uint8_t* raw = sRaw + st * F::RAW;
       ptx::mbar_wait(&raw_full[st], (t / kStages) & 1, err, kErrRaw);
       if (t >= kStages) ptx::mbar_wait(&kv_free[st], (t / kStages - 1) & 1, err, kErrFree);
       __syncwarp();
+      // (every row warp is past tile t - kStages: the place of the blocks 64 before is free)
+      if (warp == kScaleWarp && t % (kBatch / NB) == 0) {
+        take_scales(t * NB);
+        fetch_scales(t * NB + kBatch);
+      }
       const bool mixed = first + NTOK > least;      // some queries do not see all of the tile's rows
       bool odd = false;
 #pragma unroll
@@ -229,24 +259,14 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
         *reinterpret_cast<uint4*>(box + ptx::swz128(r, 2 * (p % 4))) = make_uint4(a.x, a.y, d.x, d.y);
         *reinterpret_cast<uint4*>(box + ptx::swz128(r, 2 * (p % 4) + 1)) = make_uint4(f.x, f.y, g.x, g.y);
       }
-      if (warp == kConvWarp) {
-        // a block that some queries do not see may hold nothing yet, and its scale be anything
-        if (mixed && !(fabsf(ks) < INFINITY)) ks = 1.f;
-        if (mixed && !(fabsf(vs) < INFINITY)) vs = 0.f;
-        const float lv = vs < 1.1754944e-38f ? -126.f : log2f(vs);
-        lv_top = fmaxf(lv_top, NB == 2 ? fmaxf(lv, __shfl_xor_sync(0xffffffffu, lv, 1)) : lv);
-        const bool far = lv < lv_top - kFar && !(mixed && vs == 0.f);
-        if (ct < NB) s_scale[st][ct] = make_float4(ks, lv, far ? 0.f : exp2f(-lv - kLift), 0.f);
-        const uint32_t which = __ballot_sync(0xffffffffu, far) & ((1u << NB) - 1);
-        if (ct == 0) s_odd[st] = (int)(which << 1);
-      }
+      if (ct == 0) s_odd[st] = 0;
       asm volatile("bar.sync 1, %0;" ::"n"(kConvThreads) : "memory");
       if (ct == 0 && issued < nt && *err == 0) copy(issued++);  // everybody has read the tile's bytes
-      if (t + 1 < nt) scales(t + 1);
-      if (odd) atomicOr(&s_odd[st], 1);
+      if (odd) s_odd[st] = 1;
       ptx::fence_proxy_async_smem();
       ptx::mbar_arrive_warp(&kv_full[st], lane);
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
     if (ct == 0 && *err != 0)                      // a wait ran out: the copies land before the CTA leaves
       for (int t = max(0, issued - kStages); t < issued; ++t) {
         int dummy = 0;
@@ -306,8 +326,10 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
       ptx::mbar_wait(&kv_full[st], (t / kStages) & 1, err, kErrKv);           // long since done: the scales are read here
       float4 sc[NB];
 #pragma unroll
-      for (int n = 0; n < NB; ++n) sc[n] = *const_cast<const float4*>(&s_scale[st][n]);
-      const int odd = *(volatile int*)&s_odd[st];
+      for (int n = 0; n < NB; ++n) sc[n] = *const_cast<const float4*>(&s_scale[(t * NB + n) & (2 * kBatch - 1)]);
+      int odd = *(volatile int*)&s_odd[st];
+#pragma unroll
+      for (int n = 0; n < NB; ++n) odd |= __float_as_int(sc[n].w) << n;
       ptx::tc_fence_before_sync();
       ptx::mbar_arrive_warp(&s_free[grp], lane);
       if (__any_sync(0xffffffffu, first + NTOK > limit)) {
@@ -406,7 +428,7 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
           if (top == -INFINITY) continue;
 #pragma unroll
           for (int j = 0; j < kBlock; ++j) sum += ptx::fast_exp2(fmaf(s[n * kBlock + j], f[n], off[n]) - top);
-          l_run = fmaf(sum, exp2f(top - kLift - *(volatile float*)&s_scale[st][n].y), l_run);
+          l_run = fmaf(sum, exp2f(top - kLift - *(volatile float*)&s_scale[(t * NB + n) & (2 * kBatch - 1)].y), l_run);
         }
         if (odd & 1)                               // a value that is not finite, for the queries that see it
           for (int j = first; j < min(limit, first + NTOK); ++j)

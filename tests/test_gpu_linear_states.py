@@ -69,3 +69,18 @@ def test_a_long_history(dt, d):
         if dt is F32:
             for x, y, name in ((O, want[0], "O"), *zip(grads[:3], back[:3], ("dq", "dk", "dv"))):
                 close(x[:, :, h], y[:, :, h], (name, decays[h]))
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_one_head_in_sixteen_segments(dt, d):
+    q, k, v, do, s0, ds = make(dt, 1, 7000, 1, d)
+    ld, n = torch.tensor([-0.02], device="cuda"), torch.tensor([6999], dtype=torch.int32, device="cuda")
+    O, S = solar.linear_attention_fwd(q, k, v, ld, 0.3, state0=s0, lengths=n)
+    d0 = solar.linear_attention_bwd(q, k, v, ld, 0.3, do, state0=s0, dstate=ds, lengths=n)[3]
+    a = [f64(x) for x in (q, k, v, do, s0, ds)]
+    want = ho.linear_attention(*a[:3], f64(ld), 0.3, a[4], [6999])
+    close(S, want[1], "state")
+    close(d0, ho.linear_attention_backward(*a[:3], f64(ld), 0.3, a[3], a[4], a[5], [6999])[3], "dstate0")
+    if dt is F32:
+        close(O, want[0], "O")
