@@ -383,8 +383,9 @@ solar_status_t solar_lowrank_factor_static(int B, int M, int N, int d, int r, so
  * One launch, no workspace; sums run in a fixed order, so results are reproducible bit for bit.  States and sums are
  * fp32.  bf16 storage: the decayed scores and the state as an operand of q S are rounded to bf16 (the returned state is not).
  * An input that is not finite makes the outputs of its user and head infinite or NaN from there on, and can do so for
- * up to 15 events before it.
- * An output may not overlap an input or another output (the same address is refused).
+ * up to 15 events before it (backward: of dK, dV and dstate0 in reversed time).
+ * An output may not overlap an input or another output.  (Refused: a token output at the address of a token input or of
+ * another one, and a state at the address of another state, but for ..._step's.)
  * H <= 21845; T <= 2^30; T = 0 copies state0 to state.
  * ------------------------------------------------------------------------- */
 solar_status_t solar_linear_attention_fwd(int B, int T, int H, int d, solar_dtype_t dt,
@@ -449,8 +450,11 @@ solar_status_t solar_linear_attention_step(int B, int H, int d, solar_dtype_t dt
  * what it does not see does not reach it.
  *
  * Token tensors have strides as in solar_linear_attention_fwd.  One launch each, no workspace; results are
- * reproducible bit for bit.  Sums and the softmax's statistics are fp32; the weights of the softmax enter their
- * product with V as fp16 of 2^15 times their value relative to the largest (fp32 storage: two fp16 halves).
+ * reproducible bit for bit.  O may be Q itself, with Q's strides; apart from that no output may overlap an input.
+ * Sums and the softmax's statistics are fp32.  The weights of the softmax enter their product with V as fp16: weights good to
+ * 2^-11, or to 2^-40 of the largest one where that is more (fp32 storage: two fp16 halves, 2^-22 or 2^-40).  Where bf16 queries are many
+ * (d = 64, 128; which of two kernels runs goes by estimated time, from B, M, Hq, H and N) it is the product of weight and value
+ * scale that is good to 2^-11, or to 2^-28 of the row's largest such product.
  * H <= 21845; T, M, N <= 2^30.
  * ------------------------------------------------------------------------- */
 #define SOLAR_CACHE_BLOCK 64

@@ -24,10 +24,13 @@
 //   p    2^(s - m + 15), so that fp16 holds weights down to 2^-39 of the largest; fp32 storage: high and low halves
 // The sums of a block's p V are fp32 and are scaled by the block's 2^e as they join the row's.
 //
-// 64 users, 8 query heads over 2 x 128, 8192 to 16384 rows each: 91 us with the append, 4.4 TB/s (all of 16384: 4.6); d = 64
-// 55 us.  Bound by the ALU pipe: about 1200 instructions for a warp's 64 rows of d = 128, a fifth of them conversions
-// (by shifts and masks in their place 171 us), with eight warps an SM; whence packed arithmetic, plain copies of whole
-// blocks and products of eight tiles in flight (140 us with rows straight from global memory, 107, 94).
+// 64 users, 8 query heads over 2 x 128: 92 us a launch where each has 16384 rows, 5.8 TB/s; 87 us, 4.6 TB/s, where they have 8192
+// to 16384 (90 with the append), since every user gets the same number of CTAs and the SMs are then active three quarters of
+// the time; d = 64, all of 16384, 54 us, 5.0 TB/s.  No pipe is full (issue slots 34 %, ALU 30 %, tensor 34 % of the active time):
+// latency, with two warps a scheduler at 255 registers, of about 1200 instructions for a warp's 64 rows of d = 128, a fifth of them
+// conversions (by shifts and masks in their place 171 us); products, exponentials and sums are made for 16 query rows, of which
+// a group of four heads has four.  Hence packed arithmetic, plain copies of whole blocks and products of eight tiles in flight
+// (140 us with rows straight from global memory, 107, 94).
 #include <cuda_fp16.h>
 
 #include "sm100_ptx.cuh"

@@ -10,22 +10,23 @@
 // Scales.  A query row is brought below 2 by a power of two and to fp16 (exact down to 2^-14 of its largest).  With
 // a = (that row's scores), z = a * (scale log2e 2^e ks) + log2 vs is the log of weight times value scale, and
 //   P = 2^(z - m + 3) as fp16,   Y = sum P v8,   l = sum 2^(z - m) / vs,   O = 2^-3 Y / l
-// where m is the largest z so far: P is then exact to fp16's 11 bits wherever the product of weight and value scale is
-// within 2^-17 of the row's largest (and to 2^-28 of that largest below), which is what the output is rounded by.  m is raised (Y and l rescaled) only when
-// the weights of a block add up to more than 2^15, and so before one of them is too large for fp16.
+// where m is the largest z of some tile before or of this one: P is then exact to fp16's 11 bits wherever the product of weight and value
+// scale is within 2^-17 of the row's largest (and to 2^-28 of that largest below), which is what the output is rounded by.  m is
+// raised (Y and l rescaled) only when the weights of a block add up to more than 2^15, and so before one of them is too large
+// for fp16.
 // The weights of a block whose value scale lies 2^64 or more below the largest one so far (one of zeros, whose scale is 2^-100,
 // beside values of any size) may vanish from 2^(z - m) although they count in l: such a block is added to l by exponentials
 // of its own, relative to its own maximum, and l is rescaled in two steps where m rises by more than fp32 has exponents.
 // Where the queries alone do not fill the GPU the cache's rows are split over the CTAs of a cluster, which add up through
 // distributed shared memory.  Every wait is bounded; if one runs out the tile's output rows are written as NaN.
 //
-// 16 x 2048 queries over 10240 rows: d = 64 178 us (485 TFLOP/s; 3.4e8 exponentials would take the special-function units
+// 16 x 2048 queries over 10240 rows: d = 64 170 us a launch (505 TFLOP/s; 3.4e8 exponentials would take the special-function units
 // 72), d = 128 235 us (730).  Bound by the row warps' chain of a tile, 2.2 us of wait, load, exponentials and store with two
 // warps a scheduler to hide it: without the exponentials 113, without the conversion 170, without the products 186 us
 // (d = 64, at 210 us).  Hence as little as possible in it: no maximum, no division, one fused multiplication a pair.
-#include <climits>
-
 #include <cuda_fp16.h>
+
+#include <climits>
 
 #include "sm100_ptx.cuh"
 #include "solar_internal.cuh"
@@ -193,8 +194,8 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
       bulk_load(sRaw + (t % kStages) * F::RAW, kc + (size_t)first * D, bytes, &raw_full[t % kStages]);
       bulk_load(sRaw + (t % kStages) * F::RAW + F::RAW / 2, vc + (size_t)first * D, bytes, &raw_full[t % kStages]);
     };
-    // Scales are brought and looked at by the first of these warps, 32 blocks at a time (one tile's at a time, in the path of its
-    // conversion: d = 128 250 us in the place of 229).
+    // Scales are brought and looked at by the last of these warps (which converts least), 32 blocks at a time.  A tile's own ones at a
+    // time, in the path of its conversion: d = 128 250 us in the place of 235.
     float lv_top = -INFINITY;                      // log2 of the largest value scale so far
     auto fetch_scales = [&](int from) {            // blocks of this CTA's range from .. from + 31
       const int blk = t0 * NB + from + lane;

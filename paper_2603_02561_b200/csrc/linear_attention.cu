@@ -28,7 +28,8 @@
 // (2.1 TB/s); where segments are not needed (8 x 2560, 37 heads) 104 us, 3.7 TB/s.  Bound by those chains, about 3000 cycles
 // each for 400 instructions of a warp alone on its scheduler (a CTA alone on an SM takes 1.9 us a chunk, two 2.6): mma.sync
 // is busy 41 %, shared memory 40 %, neither fewer products (-25 %) nor earlier loads moved it.  d = 128: 16 warps an SM, 3.5 to
-// 4.3 us a chunk, of which the products need 2.2.
+// 4.3 us a chunk, of which the products need 2.2 (16 x 10240, 4 heads: 510 us).  fp32 storage, 16 x 10240, 4 heads of 32, 64, 128: 273,
+// 631, 2102 us; its tiles go through registers and none is on its way while one is worked on.
 #include <cuda_bf16.h>
 
 #include <type_traits>
@@ -614,7 +615,8 @@ constexpr int kMaxSegments = 16;     // CTAs of a cluster
 // chunk; where the history is segmented 25 a chunk, the sums of its keys and values coming first, and 11 more for every CTA
 // of the cluster.  Sixteen CTAs only where all clusters find their SMs at once.  us a launch, 4 heads of 64 of one user: 200
 // events 9.6 whole, 10.2 in four; 1000 events 29, 25, 17.5, 16.4 in one, two, four, eight; 3000 events 26 in eight, 28 in
-// sixteen; 10240 events 99 in four, 46 in sixteen.
+// sixteen; 10240 events 99 in four, 46 in sixteen.  These are the times of d = 64 in bf16; d = 128 and fp32 storage take two to
+// four times as long for a chunk, segmented or not, so that the start and the cluster count for less there than they are taken for.
 template <typename F> int linear_segments(long long ctas, int T) {
   const int chunks = (T + F::C - 1) / F::C;
   const long long slots = (long long)kNumSMs * F::PER_SM;

@@ -540,7 +540,8 @@ _E4M3 = torch.float8_e4m3fn
 
 
 class HistoryCache(NamedTuple):
-    """The cache of B users: k, v [B,H,N,d] float8_e4m3fn and the scales [B,H,N/64] fp32 of their blocks of 64 rows."""
+    """The cache of B users: k, v [B,H,N,d] float8_e4m3fn and the scales [B,H,N/64] fp32 of their blocks of 64 rows (positive; the
+    append writes powers of two, and makes one of the scale of a block that it continues)."""
     k: torch.Tensor
     v: torch.Tensor
     k_scale: torch.Tensor
