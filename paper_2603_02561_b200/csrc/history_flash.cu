@@ -220,7 +220,8 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
         if (lane >= d) top = fmaxf(top, other);
       }
       lv_top = __shfl_sync(0xffffffffu, top, 31);
-      const bool far = lv < top - kFar && !(part && vs == 0.f);
+      const bool held = (t0 * NB + from + lane) * kBlock < len;
+      const bool far = held && lv < top - kFar && !(part && vs == 0.f);
       s_scale[(from & kBatch) + lane] = make_float4(ks, lv, far ? 0.f : exp2f(-lv - kLift), __int_as_float(far ? 2 : 0));
     };
     int issued = 0;
@@ -238,7 +239,7 @@ history_flash_kernel(const __grid_constant__ HistoryCall c, int splits) {
         take_scales(t * NB);
         fetch_scales(t * NB + kBatch);
       }
-      const bool mixed = first + NTOK > least;      // some queries do not see all of the tile's rows
+      const bool mixed = first + NTOK > least;     // some queries do not see all of the tile's rows
       bool odd = false;
 #pragma unroll
       for (int i = 0; i < F::PER; ++i) {
